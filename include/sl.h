@@ -262,6 +262,126 @@ sl_status sl_kv_append_fp8(const sl_attn_desc *desc, const uint16_t *k_new, cons
                            float *v_scales);
 
 /*
+ * The 4-bit cache. A pool is bytes [num_pages][num_kv_heads][17 D]: one record
+ * per page and KV head, with the page's 16 key rows and 16 value rows of that
+ * head. A row is cut into blocks of 32 consecutive elements; a block is 32 E2M1
+ * codes (sign, 2 exponent bits, 1 mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6) and
+ * one E8M0 scale byte s, and element d is e2m1(code) * 2^(s - 127), or NaN where
+ * s is 255 (the OCP MX format MXFP4, block 32). With t the token's slot in the
+ * page, d the element, C = D / 32 and E = D / 16, the record's bytes are
+ *   K code (t, d)   nibble d % 2 (0: low) of byte 256 (d / 32) + 16 t + (d % 32) / 2
+ *   V code (t, d)   nibble d % 2 of byte
+ *                   8 D + 2 E (16 (t / 4) + d / E) + (E / 2) (t % 4) + (d % E) / 2
+ *   K scale (t, c)  byte 16 D + 16 c + t
+ *   V scale (t, c)  byte 16 D + D / 2 + 4 (C (t / 4) + c) + t % 4
+ * (the order in which the attention's matrix operands are loaded). Per token and
+ * KV head that is D + D / 16 bytes for K and V, 136 for D = 128: 53% of E4M3,
+ * 27% of bf16.
+ *
+ * Rows are quantised on write. Per block, with a = max |x|: the scale is the
+ * smallest power of two 2^e with a < 7 2^e (under which a rounds to 6 or less),
+ * -126 <= e <= 125; every element is the nearest code of x / 2^e, ties to even,
+ * saturating at 6 (only from a >= 7 2^125 on). So |stored - x| <= max(|x| / 4,
+ * 2^e / 4), and exact for zeros. A block with a NaN or an infinity is stored as
+ * s = 255 with zero codes. A token owns whole bytes of a record: writing one row
+ * neither reads nor changes its neighbours.
+ *
+ * Decode attention over a 4-bit cache; the cached values are as above, and
+ * everything else (arithmetic, workspace, errors, invalid device data) is as
+ * sl_decode_attn and, with prefix sharing, sl_decode_attn_prefix.
+ *   kv_pages   uint8 [num_pages][Hkv][17 D], 16-byte aligned
+ */
+sl_status sl_decode_attn_fp4(const sl_attn_desc *desc, const uint16_t *q, const uint8_t *kv_pages,
+                             const int32_t *block_table, const int32_t *seq_lens, float scale,
+                             uint16_t *out);
+sl_status sl_decode_attn_prefix_fp4(const sl_attn_desc *desc, const uint16_t *q,
+                                    const uint8_t *kv_pages, const int32_t *block_table,
+                                    const int32_t *seq_lens, const int32_t *group_start,
+                                    const int32_t *shared_pages, int32_t num_groups, float scale,
+                                    uint16_t *out);
+
+/*
+ * KV append into a 4-bit cache: sl_kv_append with the quantise-on-write above.
+ * k_new, v_new need 16-byte alignment. Two sequences of a call may share the
+ * receiving page as long as they do not share its slot.
+ */
+sl_status sl_kv_append_fp4(const sl_attn_desc *desc, const uint16_t *k_new, const uint16_t *v_new,
+                           const int32_t *block_table, const int32_t *seq_lens, uint8_t *kv_pages);
+
+/*
+ * Rows in and out of a 4-bit cache by slot: row t belongs to slot slots[t] =
+ * page * 16 + slot in the page (a slot map as sl_pages_extend makes it), for
+ * every KV head. sl_kv_write_fp4 quantises num_tokens rows into the cache, as
+ * prefill does with a chunk of prompts; sl_kv_read_fp4 returns rows as bf16, the
+ * stored values exactly, for a dense kernel over earlier tokens.
+ *   k_new, v_new, k_out, v_out  bf16 bits [num_tokens][Hkv][D], 16-byte aligned
+ *   slots                       device int32 [num_tokens]
+ * A negative slot is no token: nothing is written, and zero rows are read. A slot
+ * of num_pages * 16 or more writes nothing and reads NaN rows. Two rows of one
+ * write that name the same slot leave it unspecified (no fault).
+ * Uses desc fields num_kv_heads, head_dim, page_size, num_pages, stream and the
+ * timing events. Errors: SL_ERR_NULL, SL_ERR_SHAPE (num_tokens < 0 among them),
+ * SL_ERR_UNSUPPORTED (also num_tokens * num_kv_heads >= 2^27 and num_pages >=
+ * 2^27), SL_ERR_ALIGNMENT, SL_ERR_HIP.
+ */
+sl_status sl_kv_write_fp4(const sl_attn_desc *desc, const uint16_t *k_new, const uint16_t *v_new,
+                          const int32_t *slots, int32_t num_tokens, uint8_t *kv_pages);
+sl_status sl_kv_read_fp4(const sl_attn_desc *desc, const uint8_t *kv_pages, const int32_t *slots,
+                         int32_t num_tokens, uint16_t *k_out, uint16_t *v_out);
+
+/*
+ * Page bookkeeping on the GPU, for a paged cache of any type: block tables and
+ * slot maps from the requests' lengths, without a trip to the host (the decode
+ * engine of sl_engine.h keeps its own on the host).
+ *
+ * The free pages are a stack: the first free_count[0] entries of free_pages,
+ * taken from and returned to its end.
+ *
+ * sl_pages_extend makes room for new_tokens[b] more tokens of every request b,
+ * whose first seq_lens[b] tokens have their pages already. In request order,
+ * request b takes ceil((L + n) / 16) - ceil(L / 16) pages from the top of the
+ * stack; they are entered in its row of the block table, and its tokens' slots
+ * (page * 16 + slot in the page) follow those of request b - 1 in the slot map.
+ * A request with a length or count that is negative or does not fit its row of
+ * the table is left as it is. So is one for which there is no room: if the new
+ * tokens of the valid requests up to b exceed max_tokens, or if it opens pages
+ * and the pages that those requests open exceed the stack. It shows: its entry in
+ * seq_lens_out is its old length, and it has no tokens between its token_start
+ * and the next.
+ *   seq_lens, new_tokens  device int32 [batch]
+ *   block_table           [batch][max_blocks_per_seq], new pages entered in place
+ *   free_pages            device int32 [num_pages]
+ *   free_count            device int32 [1] (taken as within 0 .. num_pages)
+ *   seq_lens_out          [batch] the new lengths; may be seq_lens
+ *   free_count_out        [1] pages left on the stack; may be free_count
+ *   token_start           [batch + 1] first token of each request in the slot map
+ *   slots                 [max_tokens]; -1 past the last token, and for a token
+ *                         whose page id lies outside [0, num_pages)
+ *
+ * sl_pages_release returns the pages of every request with finished[b] != 0 to
+ * the stack, request by request and a request's last block first, and sets its
+ * length to 0 (a request whose length is invalid is left as it is; pages beyond
+ * num_pages in all, which a request released twice brings, are dropped). The
+ * block table is not changed.
+ *
+ * Other than the aliases named, the arrays must not overlap. Both use desc fields
+ * batch (also 0), page_size, max_blocks_per_seq, num_pages and stream; no
+ * workspace, and the timing events are not recorded. Errors: SL_ERR_NULL,
+ * SL_ERR_SHAPE (max_tokens < 0 among them), SL_ERR_UNSUPPORTED (page_size,
+ * batch > 8192, batch * max_blocks_per_seq >= 2^28, num_pages >= 2^27,
+ * max_blocks_per_seq >= 2^27), SL_ERR_ALIGNMENT (4 bytes), SL_ERR_HIP.
+ */
+sl_status sl_pages_extend(const sl_attn_desc *desc, const int32_t *seq_lens,
+                          const int32_t *new_tokens, int32_t *block_table,
+                          const int32_t *free_pages, const int32_t *free_count, int32_t max_tokens,
+                          int32_t *seq_lens_out, int32_t *free_count_out, int32_t *token_start,
+                          int32_t *slots);
+sl_status sl_pages_release(const sl_attn_desc *desc, const int32_t *finished,
+                           const int32_t *seq_lens, const int32_t *block_table, int32_t *free_pages,
+                           const int32_t *free_count, int32_t *seq_lens_out,
+                           int32_t *free_count_out);
+
+/*
  * Decode attention with a bf16 cache that allocates nothing, for callers that
  * cannot allocate device memory: code under HIP graph capture, tight serving
  * loops, harnesses that forbid hipMalloc. Same arguments, kernels and result

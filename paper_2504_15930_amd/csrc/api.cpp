@@ -69,7 +69,7 @@ struct DeviceInfo {
     std::once_flag once;
     hipError_t err = hipSuccess;
     int cus = 0;
-    int blocks[2][2] = {{0, 0}, {0, 0}};   // [head_dim == 128][fp8]
+    int blocks[2][3] = {{0, 0, 0}, {0, 0, 0}};   // [head_dim == 128][Kv]
 };
 DeviceInfo g_devices[kMaxDevices];
 
@@ -85,8 +85,8 @@ hipError_t device_info(DeviceInfo **out)
     std::call_once(d.once, [&d, dev] {
         d.err = hipDeviceGetAttribute(&d.cus, hipDeviceAttributeMultiprocessorCount, dev);
         for (int hd = 0; hd < 2 && d.err == hipSuccess; ++hd)
-            for (int f = 0; f < 2 && d.err == hipSuccess; ++f)
-                d.err = split_blocks_per_cu(hd ? 128 : 64, f != 0, &d.blocks[hd][f]);
+            for (int kv = kBf16; kv <= kFp4 && d.err == hipSuccess; ++kv)
+                d.err = split_blocks_per_cu(hd ? 128 : 64, kv, &d.blocks[hd][kv]);
     });
     *out = &d;
     return d.err;
@@ -123,7 +123,7 @@ sl_status check_desc(const sl_attn_desc *d)
     return SL_OK;
 }
 
-sl_status resolve_workers(const sl_attn_desc *d, bool fp8, int *nw, bool prefix = false)
+sl_status resolve_workers(const sl_attn_desc *d, int kv, int *nw, bool prefix = false)
 {
     if (d->num_workers > 0) {
         *nw = d->num_workers;
@@ -143,8 +143,8 @@ sl_status resolve_workers(const sl_attn_desc *d, bool fp8, int *nw, bool prefix 
     // were slower for all but E4M3 with head_dim 64 and one tile per step.
     // Prefix-shared attention keeps one own-page workgroup per CU beside its shared-page
     // workgroups (three per four CUs was 12% slower).
-    const int blocks = info->blocks[d->head_dim == 128][fp8 ? 1 : 0];
-    const int per_cu4 = fp8 || prefix || d->head_dim == 64 ? 4 : 3;   // workgroups per four CUs
+    const int blocks = info->blocks[d->head_dim == 128][kv];
+    const int per_cu4 = kv != kBf16 || prefix || d->head_dim == 64 ? 4 : 3;   // workgroups per four CUs
     *nw = (blocks > 0 ? info->cus * per_cu4 / 4 : info->cus) * kWavesPerBlock;
     if (*nw > kMaxWorkers)
         *nw = kMaxWorkers;
@@ -164,14 +164,15 @@ bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0
 
 sl_status run(const sl_attn_desc *d, const uint16_t *q, const void *k_pages, const void *v_pages,
               const float *k_scales, const float *v_scales, const int32_t *block_table,
-              const int32_t *seq_lens, float scale, uint16_t *out, bool fp8, const AppendParams *next = nullptr)
+              const int32_t *seq_lens, float scale, uint16_t *out, int kv, const AppendParams *next = nullptr)
 {
+    const bool fp8 = kv == kE4m3;
     sl_status st = check_desc(d);
     if (st != SL_OK)
         return st;
     if (d->batch == 0)
         return SL_OK;
-    if (!q || !k_pages || !v_pages || !block_table || !seq_lens || !out)
+    if (!q || !k_pages || (!v_pages && kv != kFp4) || !block_table || !seq_lens || !out)
         return SL_ERR_NULL;
     if (fp8 && (!k_scales || !v_scales))
         return SL_ERR_NULL;
@@ -181,7 +182,7 @@ sl_status run(const sl_attn_desc *d, const uint16_t *q, const void *k_pages, con
         (fp8 && (!aligned4(k_scales) || !aligned4(v_scales))))
         return SL_ERR_ALIGNMENT;
     int nw = 0;
-    st = resolve_workers(d, fp8, &nw);
+    st = resolve_workers(d, kv, &nw);
     if (st != SL_OK)
         return st;
     const int G = d->num_q_heads / d->num_kv_heads;
@@ -218,7 +219,7 @@ sl_status run(const sl_attn_desc *d, const uint16_t *q, const void *k_pages, con
     sp.num_pages = d->num_pages;
     if (d->timing_start && hipEventRecord(d->timing_start, d->stream) != hipSuccess)
         return SL_ERR_HIP;
-    if (launch_split(sp, d->head_dim, fp8, d->stream) != hipSuccess)
+    if (launch_split(sp, d->head_dim, kv, d->stream) != hipSuccess)
         return SL_ERR_HIP;
     if (d->timing_stop && hipEventRecord(d->timing_stop, d->stream) != hipSuccess)
         return SL_ERR_HIP;
@@ -234,9 +235,9 @@ sl_status run(const sl_attn_desc *d, const uint16_t *q, const void *k_pages, con
     mp.num_kv_heads = d->num_kv_heads;
     mp.group = G;
     mp.num_workers = nw;
-    mp.step_tiles = split_step_tiles(d->head_dim, fp8);
+    mp.step_tiles = split_step_tiles(d->head_dim, kv);
     mp.group_inverse = inverse_of(G);
-    mp.fp8 = fp8;
+    mp.kv = kv;
     mp.has_next = next != nullptr;
     if (next)
         mp.next = *next;
@@ -303,14 +304,15 @@ sl_status check_prefix(const sl_attn_desc *d, int32_t num_groups)
 sl_status run_prefix(const sl_attn_desc *d, const uint16_t *q, const void *k_pages, const void *v_pages,
                      const float *k_scales, const float *v_scales, const int32_t *block_table,
                      const int32_t *seq_lens, const int32_t *group_start, const int32_t *shared_pages,
-                     int32_t num_groups, float scale, uint16_t *out, bool fp8)
+                     int32_t num_groups, float scale, uint16_t *out, int kv)
 {
+    const bool fp8 = kv == kE4m3;
     sl_status st = check_prefix(d, num_groups);
     if (st != SL_OK)
         return st;
     if (d->batch == 0)
         return SL_OK;
-    if (!q || !k_pages || !v_pages || !block_table || !seq_lens || !out ||
+    if (!q || !k_pages || (!v_pages && kv != kFp4) || !block_table || !seq_lens || !out ||
         (num_groups > 0 && (!group_start || !shared_pages)) || (fp8 && (!k_scales || !v_scales)))
         return SL_ERR_NULL;
     if (!aligned16(q) || !aligned16(out) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned4(block_table) ||
@@ -318,7 +320,7 @@ sl_status run_prefix(const sl_attn_desc *d, const uint16_t *q, const void *k_pag
         (fp8 && (!aligned4(k_scales) || !aligned4(v_scales))))
         return SL_ERR_ALIGNMENT;
     int nw = 0;
-    st = resolve_workers(d, fp8, &nw, true);
+    st = resolve_workers(d, kv, &nw, true);
     if (st != SL_OK)
         return st;
     const int G = d->num_q_heads / d->num_kv_heads;
@@ -379,7 +381,7 @@ sl_status run_prefix(const sl_attn_desc *d, const uint16_t *q, const void *k_pag
     sp_.unit_acc = ws.own_unit_acc;
     if (d->timing_start && hipEventRecord(d->timing_start, d->stream) != hipSuccess)
         return SL_ERR_HIP;
-    if (launch_prefix_split(sp_, shp, nws_max, pp, d->head_dim, fp8, d->stream) != hipSuccess)
+    if (launch_prefix_split(sp_, shp, nws_max, pp, d->head_dim, kv, d->stream) != hipSuccess)
         return SL_ERR_HIP;
     if (d->timing_stop && hipEventRecord(d->timing_stop, d->stream) != hipSuccess)
         return SL_ERR_HIP;
@@ -409,11 +411,78 @@ sl_status run_prefix(const sl_attn_desc *d, const uint16_t *q, const void *k_pag
     mp.num_shared_workers = nws;
     mp.max_shared_workers = nws_max;
     mp.max_blocks = d->max_blocks_per_seq;
-    mp.step_tiles = split_step_tiles(d->head_dim, fp8);
+    mp.step_tiles = split_step_tiles(d->head_dim, kv);
     mp.group_inverse = inverse_of(G);
-    mp.fp8 = fp8;
+    mp.kv = kv;
     if (launch_merge_prefix(mp, d->head_dim, d->stream) != hipSuccess)
         return SL_ERR_HIP;
+    return SL_OK;
+}
+
+// What the rows of a 4-bit cache need of a descriptor: heads, head_dim, pages.
+sl_status check_fp4_pool(const sl_attn_desc *d)
+{
+    if (!d)
+        return SL_ERR_NULL;
+    if (d->num_kv_heads <= 0 || d->head_dim <= 0 || d->page_size <= 0 || d->num_pages <= 0)
+        return SL_ERR_SHAPE;
+    if ((d->head_dim != 64 && d->head_dim != 128) || d->page_size != kPageSize)
+        return SL_ERR_UNSUPPORTED;
+    // Slots and page-head tile indices are 32 bits.
+    if ((long long)d->num_pages * kPageSize >= (1LL << 31) ||
+        (long long)d->num_pages * d->num_kv_heads >= (1LL << 31))
+        return SL_ERR_UNSUPPORTED;
+    return SL_OK;
+}
+
+sl_status run_fp4_rows(const sl_attn_desc *d, const Fp4RowParams &rows)
+{
+    Fp4RowParams p = rows;
+    p.num_kv_heads = d->num_kv_heads;
+    p.max_blocks = d->max_blocks_per_seq;
+    p.num_pages = d->num_pages;
+    if (d->timing_start && hipEventRecord(d->timing_start, d->stream) != hipSuccess)
+        return SL_ERR_HIP;
+    if (launch_fp4_rows(p, d->head_dim, d->stream) != hipSuccess)
+        return SL_ERR_HIP;
+    if (d->timing_stop && hipEventRecord(d->timing_stop, d->stream) != hipSuccess)
+        return SL_ERR_HIP;
+    return SL_OK;
+}
+
+// Checks of a call on `num_tokens` rows through a slot map; *run is false where there is nothing to do.
+sl_status check_fp4_slots(const sl_attn_desc *d, int32_t num_tokens, const void *k, const void *v,
+                          const int32_t *slots, const uint8_t *kv_pages, bool *run)
+{
+    *run = false;
+    sl_status st = check_fp4_pool(d);
+    if (st != SL_OK)
+        return st;
+    if (num_tokens < 0)
+        return SL_ERR_SHAPE;
+    if ((long long)num_tokens * d->num_kv_heads >= (1LL << 27))   // rows of a launch
+        return SL_ERR_UNSUPPORTED;
+    if (num_tokens == 0)
+        return SL_OK;
+    if (!k || !v || !slots || !kv_pages)
+        return SL_ERR_NULL;
+    if (!aligned16(k) || !aligned16(v) || !aligned16(kv_pages) || !aligned4(slots))
+        return SL_ERR_ALIGNMENT;
+    *run = true;
+    return SL_OK;
+}
+
+sl_status check_pages(const sl_attn_desc *d)
+{
+    if (!d)
+        return SL_ERR_NULL;
+    if (d->batch < 0 || d->page_size <= 0 || d->max_blocks_per_seq <= 0 || d->num_pages <= 0)
+        return SL_ERR_SHAPE;
+    // Positions, slots and the batch's tokens in all are 32 bits.
+    if (d->page_size != kPageSize || d->batch > kMaxBatch || (long long)d->num_pages * kPageSize >= (1LL << 31) ||
+        (long long)d->max_blocks_per_seq * kPageSize >= (1LL << 31) ||
+        (long long)d->batch * d->max_blocks_per_seq >= (1LL << 28))
+        return SL_ERR_UNSUPPORTED;
     return SL_OK;
 }
 
@@ -424,7 +493,7 @@ sl_status decode_attn_then_append(const sl_attn_desc *d, const uint16_t *q, cons
                                   const int32_t *seq_lens, float scale, uint16_t *out, bool fp8,
                                   const AppendParams *next)
 {
-    return run(d, q, k_pages, v_pages, k_scales, v_scales, block_table, seq_lens, scale, out, fp8, next);
+    return run(d, q, k_pages, v_pages, k_scales, v_scales, block_table, seq_lens, scale, out, fp8 ? kE4m3 : kBf16, next);
 }
 
 }  // namespace sl
@@ -457,7 +526,7 @@ sl_status sl_decode_attn_num_workers(const sl_attn_desc *desc, int32_t kv_fp8,
     if (!num_workers)
         return SL_ERR_NULL;
     int nw = 0;
-    st = sl::resolve_workers(desc, kv_fp8 != 0, &nw);
+    st = sl::resolve_workers(desc, kv_fp8 != 0 ? sl::kE4m3 : sl::kBf16, &nw);
     if (st == SL_OK)
         *num_workers = nw;
     return st;
@@ -489,7 +558,7 @@ sl_status sl_decode_attn(const sl_attn_desc *desc, const uint16_t *q, const uint
                          const int32_t *seq_lens, float scale, uint16_t *out)
 {
     return sl::run(desc, q, k_pages, v_pages, nullptr, nullptr, block_table, seq_lens, scale, out,
-                   false);
+                   sl::kBf16);
 }
 
 sl_status sl_decode_attn_fp8(const sl_attn_desc *desc, const uint16_t *q, const uint8_t *k_pages,
@@ -498,7 +567,7 @@ sl_status sl_decode_attn_fp8(const sl_attn_desc *desc, const uint16_t *q, const 
                              uint16_t *out)
 {
     return sl::run(desc, q, k_pages, v_pages, k_scales, v_scales, block_table, seq_lens, scale,
-                   out, true);
+                   out, sl::kE4m3);
 }
 
 const char *sl_status_string(int32_t status)
@@ -559,6 +628,141 @@ sl_status sl_decode_attn_prefix_fp8(const sl_attn_desc *desc, const uint16_t *q,
 {
     return sl::run_prefix(desc, q, k_pages, v_pages, k_scales, v_scales, block_table, seq_lens, group_start,
                           shared_pages, num_groups, scale, out, true);
+}
+
+sl_status sl_decode_attn_fp4(const sl_attn_desc *desc, const uint16_t *q, const uint8_t *kv_pages,
+                             const int32_t *block_table, const int32_t *seq_lens, float scale, uint16_t *out)
+{
+    return sl::run(desc, q, kv_pages, nullptr, nullptr, nullptr, block_table, seq_lens, scale, out, sl::kFp4);
+}
+
+sl_status sl_decode_attn_prefix_fp4(const sl_attn_desc *desc, const uint16_t *q, const uint8_t *kv_pages,
+                                    const int32_t *block_table, const int32_t *seq_lens, const int32_t *group_start,
+                                    const int32_t *shared_pages, int32_t num_groups, float scale, uint16_t *out)
+{
+    return sl::run_prefix(desc, q, kv_pages, nullptr, nullptr, nullptr, block_table, seq_lens, group_start,
+                          shared_pages, num_groups, scale, out, sl::kFp4);
+}
+
+sl_status sl_kv_append_fp4(const sl_attn_desc *desc, const uint16_t *k_new, const uint16_t *v_new,
+                           const int32_t *block_table, const int32_t *seq_lens, uint8_t *kv_pages)
+{
+    sl_status st = sl::check_desc(desc);
+    if (st == SL_OK)
+        st = sl::check_fp4_pool(desc);
+    if (st != SL_OK)
+        return st;
+    if (desc->batch == 0)
+        return SL_OK;
+    if (!k_new || !v_new || !block_table || !seq_lens || !kv_pages)
+        return SL_ERR_NULL;
+    if (!sl::aligned16(k_new) || !sl::aligned16(v_new) || !sl::aligned16(kv_pages) || !sl::aligned4(block_table) ||
+        !sl::aligned4(seq_lens))
+        return SL_ERR_ALIGNMENT;
+    sl::Fp4RowParams p = {};
+    p.k_rows = k_new;
+    p.v_rows = v_new;
+    p.block_table = block_table;
+    p.seq_lens = seq_lens;
+    p.pages = kv_pages;
+    p.rows = desc->batch;
+    return sl::run_fp4_rows(desc, p);
+}
+
+sl_status sl_kv_write_fp4(const sl_attn_desc *desc, const uint16_t *k_new, const uint16_t *v_new,
+                          const int32_t *slots, int32_t num_tokens, uint8_t *kv_pages)
+{
+    bool run = false;
+    const sl_status st = sl::check_fp4_slots(desc, num_tokens, k_new, v_new, slots, kv_pages, &run);
+    if (st != SL_OK || !run)
+        return st;
+    sl::Fp4RowParams p = {};
+    p.k_rows = k_new;
+    p.v_rows = v_new;
+    p.slots = slots;
+    p.pages = kv_pages;
+    p.rows = num_tokens;
+    return sl::run_fp4_rows(desc, p);
+}
+
+sl_status sl_kv_read_fp4(const sl_attn_desc *desc, const uint8_t *kv_pages, const int32_t *slots,
+                         int32_t num_tokens, uint16_t *k_out, uint16_t *v_out)
+{
+    bool run = false;
+    const sl_status st = sl::check_fp4_slots(desc, num_tokens, k_out, v_out, slots, kv_pages, &run);
+    if (st != SL_OK || !run)
+        return st;
+    sl::Fp4RowParams p = {};
+    p.k_out = k_out;
+    p.v_out = v_out;
+    p.slots = slots;
+    p.pages = const_cast<uint8_t *>(kv_pages);
+    p.rows = num_tokens;
+    return sl::run_fp4_rows(desc, p);
+}
+
+sl_status sl_pages_extend(const sl_attn_desc *desc, const int32_t *seq_lens, const int32_t *new_tokens,
+                          int32_t *block_table, const int32_t *free_pages, const int32_t *free_count,
+                          int32_t max_tokens, int32_t *seq_lens_out, int32_t *free_count_out, int32_t *token_start,
+                          int32_t *slots)
+{
+    const sl_status st = sl::check_pages(desc);
+    if (st != SL_OK)
+        return st;
+    if (max_tokens < 0)
+        return SL_ERR_SHAPE;
+    if (!free_count || !free_count_out || !token_start || (max_tokens > 0 && !slots) ||
+        (desc->batch > 0 && (!seq_lens || !new_tokens || !block_table || !free_pages || !seq_lens_out)))
+        return SL_ERR_NULL;
+    for (const void *a : {(const void *)seq_lens, (const void *)new_tokens, (const void *)block_table,
+                          (const void *)free_pages, (const void *)free_count, (const void *)seq_lens_out,
+                          (const void *)free_count_out, (const void *)token_start, (const void *)slots})
+        if (!sl::aligned4(a))
+            return SL_ERR_ALIGNMENT;
+    sl::PageParams p = {};
+    p.seq_lens = seq_lens;
+    p.new_tokens = new_tokens;
+    p.block_table = block_table;
+    p.free_pages = const_cast<int32_t *>(free_pages);
+    p.free_count = free_count;
+    p.seq_lens_out = seq_lens_out;
+    p.free_count_out = free_count_out;
+    p.token_start = token_start;
+    p.slots = slots;
+    p.batch = desc->batch;
+    p.max_blocks = desc->max_blocks_per_seq;
+    p.num_pages = desc->num_pages;
+    p.max_tokens = max_tokens;
+    return sl::launch_extend_pages(p, desc->stream) == hipSuccess ? SL_OK : SL_ERR_HIP;
+}
+
+sl_status sl_pages_release(const sl_attn_desc *desc, const int32_t *finished, const int32_t *seq_lens,
+                           const int32_t *block_table, int32_t *free_pages, const int32_t *free_count,
+                           int32_t *seq_lens_out, int32_t *free_count_out)
+{
+    const sl_status st = sl::check_pages(desc);
+    if (st != SL_OK)
+        return st;
+    if (!free_count || !free_count_out ||
+        (desc->batch > 0 && (!finished || !seq_lens || !block_table || !free_pages || !seq_lens_out)))
+        return SL_ERR_NULL;
+    for (const void *a : {(const void *)finished, (const void *)seq_lens, (const void *)block_table,
+                          (const void *)free_pages, (const void *)free_count, (const void *)seq_lens_out,
+                          (const void *)free_count_out})
+        if (!sl::aligned4(a))
+            return SL_ERR_ALIGNMENT;
+    sl::PageParams p = {};
+    p.finished = finished;
+    p.seq_lens = seq_lens;
+    p.block_table = const_cast<int32_t *>(block_table);
+    p.free_pages = free_pages;
+    p.free_count = free_count;
+    p.seq_lens_out = seq_lens_out;
+    p.free_count_out = free_count_out;
+    p.batch = desc->batch;
+    p.max_blocks = desc->max_blocks_per_seq;
+    p.num_pages = desc->num_pages;
+    return sl::launch_release_pages(p, desc->stream) == hipSuccess ? SL_OK : SL_ERR_HIP;
 }
 
 }  // extern "C"

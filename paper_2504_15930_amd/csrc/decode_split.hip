@@ -27,44 +27,44 @@ __global__ __launch_bounds__(kWave * kWavesPerBlock) void split_kv_kernel(SplitP
                                          StreamLds{s_cum, s_len});
 }
 
+SplitKernel split_kernel(int head_dim, int kv)
+{
+    if (kv == kFp4)
+        return split_fp4_kernel_of(head_dim);
+    if (head_dim == 128)
+        return kv == kE4m3 ? split_kv_kernel<128, true> : split_kv_kernel<128, false>;
+    if (head_dim == 64)
+        return kv == kE4m3 ? split_kv_kernel<64, true> : split_kv_kernel<64, false>;
+    return nullptr;
+}
+
 }  // namespace
 
-hipError_t launch_split(const SplitParams &p, int head_dim, bool fp8, hipStream_t stream)
+hipError_t launch_split(const SplitParams &p, int head_dim, int kv, hipStream_t stream)
 {
     const dim3 grid((p.num_workers + kWavesPerBlock - 1) / kWavesPerBlock);
     const dim3 block(kWave * kWavesPerBlock);
-    const size_t lds = split_dynamic_lds(p.batch);
-    if (head_dim == 128 && !fp8)
-        hipLaunchKernelGGL((split_kv_kernel<128, false>), grid, block, lds, stream, p);
-    else if (head_dim == 64 && !fp8)
-        hipLaunchKernelGGL((split_kv_kernel<64, false>), grid, block, lds, stream, p);
-    else if (head_dim == 128 && fp8)
-        hipLaunchKernelGGL((split_kv_kernel<128, true>), grid, block, lds, stream, p);
-    else if (head_dim == 64 && fp8)
-        hipLaunchKernelGGL((split_kv_kernel<64, true>), grid, block, lds, stream, p);
-    else
+    const SplitKernel kernel = split_kernel(head_dim, kv);
+    if (!kernel)
         return hipErrorInvalidValue;
+    hipLaunchKernelGGL(kernel, grid, block, split_dynamic_lds(p.batch), stream, p);
     return hipGetLastError();
 }
 
-hipError_t split_blocks_per_cu(int head_dim, bool fp8, int *blocks)
+hipError_t split_blocks_per_cu(int head_dim, int kv, int *blocks)
 {
-    const int threads = kWave * kWavesPerBlock;
-    if (head_dim == 128 && !fp8)
-        return hipOccupancyMaxActiveBlocksPerMultiprocessor(blocks, split_kv_kernel<128, false>, threads, 0);
-    if (head_dim == 64 && !fp8)
-        return hipOccupancyMaxActiveBlocksPerMultiprocessor(blocks, split_kv_kernel<64, false>, threads, 0);
-    if (head_dim == 128 && fp8)
-        return hipOccupancyMaxActiveBlocksPerMultiprocessor(blocks, split_kv_kernel<128, true>, threads, 0);
-    if (head_dim == 64 && fp8)
-        return hipOccupancyMaxActiveBlocksPerMultiprocessor(blocks, split_kv_kernel<64, true>, threads, 0);
-    return hipErrorInvalidValue;
+    const SplitKernel kernel = split_kernel(head_dim, kv);
+    if (!kernel)
+        return hipErrorInvalidValue;
+    return hipOccupancyMaxActiveBlocksPerMultiprocessor(blocks, kernel, kWave * kWavesPerBlock, 0);
 }
 
-int split_step_tiles(int head_dim, bool fp8)
+int split_step_tiles(int head_dim, int kv)
 {
-    return head_dim == 64 ? (fp8 ? step_tiles<64, true>() : step_tiles<64, false>())
-                          : (fp8 ? step_tiles<128, true>() : step_tiles<128, false>());
+    const bool d64 = head_dim == 64;
+    return kv == kFp4    ? d64 ? step_tiles<64, kFp4>() : step_tiles<128, kFp4>()
+           : kv == kE4m3 ? d64 ? step_tiles<64, kE4m3>() : step_tiles<128, kE4m3>()
+                         : d64 ? step_tiles<64, kBf16>() : step_tiles<128, kBf16>();
 }
 
 }  // namespace sl

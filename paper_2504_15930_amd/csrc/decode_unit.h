@@ -42,6 +42,15 @@
 // (v_cvt_scalef32_pk_bf16_fp8 with unit scale), the per-(page, head) key
 // scale multiplies the fp32 scores and the value scale multiplies the
 // probabilities before they are rounded for the value MFMA.
+//
+// FP4 records (kFp4, fp4_unit.h) hold a tile's E2M1 codes in the order of the
+// MFMA operands themselves, K and V of one tile side by side: lane (n, quad)
+// finds its part of the score operand in one 16-byte load and its four value
+// rows in another, each a whole 1 KB run (D = 128), and nothing goes through
+// LDS. The codes are widened to bf16 with their block's power of two
+// (v_cvt_scalef32_pk_bf16_fp4, exact), so scores and weights are as for a bf16
+// cache.
+#include "fp4_unit.h"
 #include "sl_internal.h"
 #include "wave_ops.h"
 
@@ -75,8 +84,8 @@ constexpr float kRescaleSlack = 8.0f;
 //   E4M3 D = 64, 384 x 1..4096 tokens, 8 KV heads   226 -> 146 us (two tiles: 157)
 // Two steps in flight; three were no faster anywhere (and slower where they
 // cost a resident workgroup, in the prefix kernel).
-template <int D, bool FP8>
-constexpr int step_tiles() { return D == 64 ? (FP8 ? 4 : 2) : (FP8 ? 2 : 1); }
+template <int D, int KV>
+constexpr int step_tiles() { return KV == kFp4 ? 4 : D == 64 ? (KV == kE4m3 ? 4 : 2) : (KV == kE4m3 ? 2 : 1); }
 constexpr int kPipelineDepth = 2;
 constexpr int kRawBufferWord3 = 0x00020000;  // untyped 32-bit buffer resource (CDNA3/4)
 
@@ -112,30 +121,39 @@ __device__ __forceinline__ float quad_sum(float x)
     return x + __shfl_xor(x, 32, kWave);
 }
 
-template <int D, bool FP8>
+template <int D, int KV>
 struct Tile {
     // Per-lane dwords of K (score-MFMA A operands) and V (four rows).
-    static constexpr int KW = FP8 ? D / 16 : D / 8;
-    static constexpr int VW = FP8 ? D / 16 : D / 8;
+    static constexpr int KW = KV == kE4m3 ? D / 16 : D / 8;
+    static constexpr int VW = KV == kE4m3 ? D / 16 : D / 8;
     uint32_t k[KW];
     uint32_t v[VW];
     float scl;           // FP8: key scale in lanes 0-31, value scale in lanes 32-63
 };
+template <int D>
+struct Tile<D, kFp4> {
+    static constexpr int KW = D / 32;
+    static constexpr int VW = D / 32;
+    uint32_t k[KW];
+    uint32_t v[VW];
+    uint32_t ks;         // the scale byte of the lane's key elements
+    uint32_t vs;         // those of its value elements in rows 4 quad + r, byte r
+};
 
 // One pipeline step: NT consecutive tiles of one unit (fewer at the unit's end).
-template <int D, bool FP8, int NT>
+template <int D, int KV, int NT>
 struct Step {
-    Tile<D, FP8> t[NT];
+    Tile<D, KV> t[NT];
     u32x4_t q[D / 32];   // the unit's query rows, loaded with a unit's first step only
     uint32_t meta;       // metadata (kMeta* bits, wave-uniform)
     int32_t valid;       // live tokens of the step, 1 .. 16 NT; kSharedPages: | (members - 1) << 8
 };
 
 // Query element index held by (quad, item) in k-step s; must match k_operand.
-template <int D, bool FP8>
+template <int D, int KV>
 __device__ __forceinline__ int q_index(int s, int quad)
 {
-    return FP8 ? quad * (D / 4) + 8 * s : 32 * s + 8 * quad;
+    return KV == kBf16 ? 32 * s + 8 * quad : quad * (D / 4) + 8 * s;
 }
 
 // K/V pages are read exactly once per call: stream them with non-temporal loads
@@ -151,7 +169,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *base, ui
 // The score-MFMA B operands of a unit with first query row row0, zero where
 // `with_q` is false: lane (n, quad) takes query row n, and the rows past the
 // group's G lie past the resource's end, so they are zero too.
-template <int D, bool FP8>
+template <int D, int KV>
 __device__ __forceinline__ void load_q(u32x4_t (&q)[D / 32], const SplitParams &p, uint32_t row0, bool with_q, int n,
                                        int quad)
 {
@@ -159,7 +177,7 @@ __device__ __forceinline__ void load_q(u32x4_t (&q)[D / 32], const SplitParams &
 #pragma unroll
     for (int s = 0; s < D / 32; ++s)
         q[s] = __builtin_bit_cast(
-            u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(qr, 2 * (n * D + q_index<D, FP8>(s, quad)), 0, 0));
+            u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(qr, 2 * (n * D + q_index<D, KV>(s, quad)), 0, 0));
 }
 
 // Issue the K/V loads of one tile (page-head tile index `tile`), always the
@@ -173,12 +191,12 @@ __device__ __forceinline__ void load_q(u32x4_t (&q)[D / 32], const SplitParams &
 // K/V are streamed with non-temporal loads (STREAM) unless the tile is read by
 // several wavefronts at once (the column blocks of a shared unit), where plain
 // loads let the siblings find it in L2.
-template <int D, bool FP8, bool STREAM>
-__device__ __forceinline__ void issue_tile(Tile<D, FP8> &t, const SplitParams &p, uint32_t tile_index, bool read,
+template <int D, int KV, bool STREAM>
+__device__ __forceinline__ void issue_tile(Tile<D, KV> &t, const SplitParams &p, uint32_t tile_index, bool read,
                                            int n, int quad, int lane)
 {
     constexpr int kPolicy = STREAM ? kCachePolicyStream : 0;
-    constexpr uint32_t kTileBytes = kPageSize * D * (FP8 ? 1 : 2);
+    constexpr uint32_t kTileBytes = kPageSize * D * (KV == kE4m3 ? 1 : 2);
     const size_t tile = tile_index;
     const __amdgpu_buffer_rsrc_t kt =
         buffer_of(static_cast<const uint8_t *>(p.k_pages) + tile * kTileBytes, read ? kTileBytes : 0u);
@@ -188,7 +206,7 @@ __device__ __forceinline__ void issue_tile(Tile<D, FP8> &t, const SplitParams &p
     // run), so every instruction covers complete 128-byte lines; the rows are
     // regrouped into the score-MFMA layout through LDS when the tile is used.
 #pragma unroll
-    for (int i = 0; i < Tile<D, FP8>::KW / 4; ++i) {
+    for (int i = 0; i < Tile<D, KV>::KW / 4; ++i) {
         const u32x4_t x = __builtin_bit_cast(
             u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(kt, 16 * lane + 1024 * i, 0, kPolicy));
 #pragma unroll
@@ -196,7 +214,7 @@ __device__ __forceinline__ void issue_tile(Tile<D, FP8> &t, const SplitParams &p
             t.k[4 * i + c] = x[c];
     }
     // V: lane (n, quad) reads D/16 consecutive elements of rows 4 quad + r.
-    constexpr int kRow = D * (FP8 ? 1 : 2);
+    constexpr int kRow = D * (KV == kE4m3 ? 1 : 2);
     const int voff = 4 * quad * kRow + n * (kRow / 16);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -216,10 +234,46 @@ __device__ __forceinline__ void issue_tile(Tile<D, FP8> &t, const SplitParams &p
                                         __builtin_amdgcn_raw_buffer_load_b32(vt, voff + r * kRow, 0, kPolicy));
         }
     }
-    if constexpr (FP8) {
+    if constexpr (KV == kE4m3) {
         const float *sp = (lane & 32) ? p.v_scales : p.k_scales;
         t.scl = sp[tile];
     }
+}
+
+// The same of an FP4 record: codes as operands lie in it, and the lane's scales.
+template <int D, bool STREAM>
+__device__ __forceinline__ void issue_record(Tile<D, kFp4> &t, const SplitParams &p, uint32_t tile, bool read, int n,
+                                             int quad, int lane)
+{
+    constexpr int kPolicy = STREAM ? kCachePolicyStream : 0;
+    using L = Fp4Layout<D>;
+    const __amdgpu_buffer_rsrc_t rec = buffer_of(static_cast<const uint8_t *>(p.k_pages) + (size_t)tile * L::kBytes,
+                                                 read ? (uint32_t)L::kBytes : 0u);
+    if constexpr (D == 128) {
+        const u32x4_t k =
+            __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rec, 16 * lane, 0, kPolicy));
+        const u32x4_t v =
+            __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rec, L::kV + 16 * lane, 0, kPolicy));
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            t.k[c] = k[c];
+            t.v[c] = v[c];
+        }
+    } else {   // half a block of 32 key elements per lane
+        const u32x2_t k = __builtin_bit_cast(
+            u32x2_t,
+            __builtin_amdgcn_raw_buffer_load_b64(rec, L::k_code(n, quad >> 1) + 8 * (quad & 1), 0, kPolicy));
+        const u32x2_t v =
+            __builtin_bit_cast(u32x2_t, __builtin_amdgcn_raw_buffer_load_b64(rec, L::kV + 8 * lane, 0, kPolicy));
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            t.k[c] = k[c];
+            t.v[c] = v[c];
+        }
+    }
+    t.ks = __builtin_amdgcn_raw_buffer_load_b8(rec, L::k_scale(n, D == 128 ? quad : quad >> 1), 0, kPolicy);
+    t.vs = __builtin_bit_cast(
+        uint32_t, __builtin_amdgcn_raw_buffer_load_b32(rec, L::v_scale(4 * quad, n * (D / 16) / 32), 0, kPolicy));
 }
 
 // Issue the loads of a step: tiles T[u] (a page-head tile index, or the
@@ -229,13 +283,18 @@ __device__ __forceinline__ void issue_tile(Tile<D, FP8> &t, const SplitParams &p
 // `blk` < 0: a single-unit step, whose query rows are the group's G heads;
 // `blk` >= 0: column block blk of a shared unit (rows 16 blk + n, member r / G
 // and head r % G of the group).
-template <int D, bool FP8, int NT, bool STREAM>
-__device__ __forceinline__ void issue_step(Step<D, FP8, NT> &st, const SplitParams &p, const int32_t (&T)[NT],
+template <int D, int KV, int NT, bool STREAM>
+__device__ __forceinline__ void issue_step(Step<D, KV, NT> &st, const SplitParams &p, const int32_t (&T)[NT],
                                            bool live, bool with_q, int n, int quad, int lane, int blk)
 {
 #pragma unroll
-    for (int u = 0; u < NT; ++u)
-        issue_tile<D, FP8, STREAM>(st.t[u], p, (uint32_t)(T[u] ^ (T[u] >> 31)), live && T[u] >= 0, n, quad, lane);
+    for (int u = 0; u < NT; ++u) {
+        const uint32_t at = (uint32_t)(T[u] ^ (T[u] >> 31));
+        if constexpr (KV == kFp4)
+            issue_record<D, STREAM>(st.t[u], p, at, live && T[u] >= 0, n, quad, lane);
+        else
+            issue_tile<D, KV, STREAM>(st.t[u], p, at, live && T[u] >= 0, n, quad, lane);
+    }
     const uint32_t row0 = (st.meta >> kMetaUnitShift) * (uint32_t)p.group;
     if (blk < 0) {
         // One tile per step: the q loads are issued only where they read
@@ -245,7 +304,7 @@ __device__ __forceinline__ void issue_step(Step<D, FP8, NT> &st, const SplitPara
         // step once per unit, which costs the others more (D = 64 bf16, 130
         // against 137 us; E4M3 D = 128, 313 against 316).
         if (NT > 1 || with_q)
-            load_q<D, FP8>(st.q, p, row0, with_q, n, quad);
+            load_q<D, KV>(st.q, p, row0, with_q, n, quad);
     } else if (with_q) {
         // Issued for a unit's first step only: four wavefronts load every tile
         // here, from L2, and with two such workgroups on a CU the load
@@ -261,7 +320,7 @@ __device__ __forceinline__ void issue_step(Step<D, FP8, NT> &st, const SplitPara
         for (int s = 0; s < D / 32; ++s)
             st.q[s] = __builtin_bit_cast(
                 u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(
-                             qr, (int)(2u * (rel * (uint32_t)D + (uint32_t)q_index<D, FP8>(s, quad))), 0, 0));
+                             qr, (int)(2u * (rel * (uint32_t)D + (uint32_t)q_index<D, KV>(s, quad))), 0, 0));
     }
 }
 
@@ -281,37 +340,37 @@ __device__ __forceinline__ void issue_step(Step<D, FP8, NT> &st, const SplitPara
 // 186 us instead of 155; 256 sequences of 1..2048 tokens with 4096 workers 74
 // instead of 65. With 4096 sequences in more than 3862 groups the prefix kernel no
 // longer fitted a CU at all.)
-template <int D, bool FP8, int NT, int N>
-__device__ __forceinline__ void regroup_k(const Tile<D, FP8> (&t)[N], uint8_t *lds, int lane, int n, int quad,
-                                          u32x4_t (&kc)[NT][FP8 ? D / 64 : D / 32])
+template <int D, int KV, int NT, int N>
+__device__ __forceinline__ void regroup_k(const Tile<D, KV> (&t)[N], uint8_t *lds, int lane, int n, int quad,
+                                          u32x4_t (&kc)[NT][KV == kE4m3 ? D / 64 : D / 32])
 {
-    constexpr int R = D * (FP8 ? 1 : 2);   // bytes per row
+    constexpr int R = D * (KV == kE4m3 ? 1 : 2);   // bytes per row
     constexpr int C = R / 16;               // 16-byte chunks per row
     constexpr int P = 256 / R;              // rows per 256 bytes
     const int key = (n / P) % C;
 #pragma unroll
     for (int u = 0; u < NT; ++u) {
 #pragma unroll
-        for (int i = 0; i < Tile<D, FP8>::KW / 4; ++i) {
+        for (int i = 0; i < Tile<D, KV>::KW / 4; ++i) {
             const int off = 1024 * i + 16 * lane;
             const int r = off / R, c = (off % R) / 16;
             *reinterpret_cast<u32x4_t *>(lds + r * R + 16 * (c ^ ((r / P) % C))) =
                 u32x4_t{t[u].k[4 * i], t[u].k[4 * i + 1], t[u].k[4 * i + 2], t[u].k[4 * i + 3]};
         }
 #pragma unroll
-        for (int s = 0; s < (FP8 ? D / 64 : D / 32); ++s) {
-            const int c = FP8 ? quad * (D / 64) + s : 4 * s + quad;
+        for (int s = 0; s < (KV == kE4m3 ? D / 64 : D / 32); ++s) {
+            const int c = KV == kE4m3 ? quad * (D / 64) + s : 4 * s + quad;
             kc[u][s] = *reinterpret_cast<const u32x4_t *>(lds + n * R + 16 * (c ^ key));
         }
     }
 }
 
 // Score-MFMA A operand for k-step s (8 bf16 values of row t = n).
-template <int D, bool FP8>
-__device__ __forceinline__ bf16x8_t k_operand(const u32x4_t (&kc)[FP8 ? D / 64 : D / 32], int s)
+template <int D, int KV>
+__device__ __forceinline__ bf16x8_t k_operand(const u32x4_t (&kc)[KV == kE4m3 ? D / 64 : D / 32], int s)
 {
     u32x4_t w;
-    if constexpr (!FP8) {
+    if constexpr (KV == kBf16) {
         w = kc[s];
     } else {
         const uint32_t lo = kc[s / 2][2 * (s % 2)], hi = kc[s / 2][2 * (s % 2) + 1];
@@ -321,6 +380,14 @@ __device__ __forceinline__ bf16x8_t k_operand(const u32x4_t (&kc)[FP8 ? D / 64 :
         w = u32x4_t{a, b, c, d};
     }
     return __builtin_bit_cast(bf16x8_t, w);
+}
+
+// The same for an FP4 record: dword s of the lane's codes, with their block's scale.
+template <int D>
+__device__ __forceinline__ bf16x8_t k_operand_fp4(const Tile<D, kFp4> &t, float scale, int s)
+{
+    return __builtin_bit_cast(bf16x8_t, u32x4_t{fp4x2_to_bf16<0>(t.k[s], scale), fp4x2_to_bf16<1>(t.k[s], scale),
+                                                fp4x2_to_bf16<2>(t.k[s], scale), fp4x2_to_bf16<3>(t.k[s], scale)});
 }
 
 template <int D>
@@ -349,23 +416,32 @@ __device__ __forceinline__ void reset(Piece<D> &st)
 // stands for token 4 quad + (i & 3) of tile i / 4 in both operands, so the
 // weights enter exactly as the score MFMAs left them, as with one tile and
 // v_mfma_f32_16x16x16bf16_1k.
-template <int D, bool FP8, int NT, int N>
-__device__ __forceinline__ void compute_step(Piece<D> &st, const Tile<D, FP8> (&t)[N],
+template <int D, int KV, int NT, int N>
+__device__ __forceinline__ void compute_step(Piece<D> &st, const Tile<D, KV> (&t)[N],
                                              const bf16x8_t (&qop)[D / 32], float score_mul, int valid, uint8_t *lds,
                                              int lane, int n, int quad)
 {
     static_assert(NT == 1 || NT % 2 == 0, "one tile, or pairs of tiles, per step");
-    u32x4_t kc[NT][FP8 ? D / 64 : D / 32];
-    regroup_k<D, FP8, NT>(t, lds, lane, n, quad, kc);
     f32x4_t s4[NT];
 #pragma unroll
     for (int u = 0; u < NT; ++u)
         s4[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    if constexpr (KV == kFp4) {
 #pragma unroll
-    for (int s = 0; s < D / 32; ++s)
+        for (int s = 0; s < D / 32; ++s)
 #pragma unroll
-        for (int u = 0; u < NT; ++u)
-            s4[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k_operand<D, FP8>(kc[u], s), qop[s], s4[u], 0, 0, 0);
+            for (int u = 0; u < NT; ++u)
+                s4[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k_operand_fp4<D>(t[u], e8m0(t[u].ks), s), qop[s], s4[u],
+                                                                0, 0, 0);
+    } else {
+        u32x4_t kc[NT][KV == kE4m3 ? D / 64 : D / 32];
+        regroup_k<D, KV, NT>(t, lds, lane, n, quad, kc);
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s)
+#pragma unroll
+            for (int u = 0; u < NT; ++u)
+                s4[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k_operand<D, KV>(kc[u], s), qop[s], s4[u], 0, 0, 0);
+    }
 
     float vmul[NT];
     float sc[NT][4];
@@ -373,7 +449,7 @@ __device__ __forceinline__ void compute_step(Piece<D> &st, const Tile<D, FP8> (&
     for (int u = 0; u < NT; ++u) {
         float mul = score_mul;
         vmul[u] = 1.0f;
-        if constexpr (FP8) {
+        if constexpr (KV == kE4m3) {
             const int bits = __builtin_bit_cast(int, t[u].scl);
             mul *= __builtin_bit_cast(float, __builtin_amdgcn_readlane(bits, 0));
             vmul[u] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(bits, 32));
@@ -391,7 +467,7 @@ __device__ __forceinline__ void compute_step(Piece<D> &st, const Tile<D, FP8> (&
                     sc[u][r] = kNegInf;
             // A missing tile carries the first one's scales: its zero weights must
             // stay zero where that value scale is infinite.
-            if (FP8 && kPageSize * u >= valid)
+            if (KV == kE4m3 && kPageSize * u >= valid)
                 vmul[u] = 1.0f;
         }
     }
@@ -428,7 +504,7 @@ __device__ __forceinline__ void compute_step(Piece<D> &st, const Tile<D, FP8> (&
 #pragma unroll
         for (int r = 0; r < 4; ++r)
             pr[r] = __builtin_amdgcn_exp2f(sc[u][r] - st.m);
-        if constexpr (FP8) {
+        if constexpr (KV == kE4m3) {
             const uint32_t w01 = pack_bf16(pr[0] * vmul[u], pr[1] * vmul[u]);
             const uint32_t w23 = pack_bf16(pr[2] * vmul[u], pr[3] * vmul[u]);
             pw[u][0] = w01;
@@ -457,28 +533,53 @@ __device__ __forceinline__ void compute_step(Piece<D> &st, const Tile<D, FP8> (&
     // rows before one widening per two blocks. Dead slots (only in a
     // sequence's last page) hold arbitrary cache contents and are zeroed first,
     // as 0 * NaN would poison the MFMA.
-    constexpr int VR = Tile<D, FP8>::VW / 4;   // dwords per row
+    // FP4 codes are finite whatever they are, and a dead slot's are only kept from
+    // an infinite or NaN scale: it takes the scale 1.
+    constexpr int VR = KV == kFp4 ? 1 : Tile<D, KV>::VW / 4;   // dwords per row
     uint32_t vr[NT][4 * VR];
-#pragma unroll
-    for (int u = 0; u < NT; ++u)
-#pragma unroll
-        for (int k = 0; k < 4 * VR; ++k)
-            vr[u][k] = t[u].v[k];
-    if (valid < kPageSize * NT) {
+    float vscale[NT][4];   // FP4: of the lane's block in each row
+    if constexpr (KV == kFp4) {
 #pragma unroll
         for (int u = 0; u < NT; ++u)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
+            for (int r = 0; r < 4; ++r) {
+                vscale[u][r] = e8m0(t[u].vs >> (8 * r));
+                if (valid < kPageSize * NT && kPageSize * u + 4 * quad + r >= valid)
+                    vscale[u][r] = 1.0f;
+                vr[u][r] = D == 128 ? t[u].v[r] : t[u].v[r / 2] >> (16 * (r % 2));
+            }
+    } else {
 #pragma unroll
-                for (int c = 0; c < VR; ++c)
-                    vr[u][r * VR + c] = kPageSize * u + 4 * quad + r < valid ? vr[u][r * VR + c] : 0u;
+        for (int u = 0; u < NT; ++u)
+#pragma unroll
+            for (int k = 0; k < 4 * VR; ++k)
+                vr[u][k] = t[u].v[k];
+        if (valid < kPageSize * NT) {
+#pragma unroll
+            for (int u = 0; u < NT; ++u)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int c = 0; c < VR; ++c)
+                        vr[u][r * VR + c] = kPageSize * u + 4 * quad + r < valid ? vr[u][r * VR + c] : 0u;
+        }
     }
 #pragma unroll
     for (int i = 0; i < D / 16; i += 2) {
         uint32_t a0[2 * NT], a1[2 * NT];   // operands of blocks i and i + 1
 #pragma unroll
         for (int u = 0; u < NT; ++u) {
-            if constexpr (FP8) {
+            if constexpr (KV == kFp4) {
+                // A byte holds elements i and i + 1 of a row.
+                uint32_t w[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    w[r] = fp4x2_to_bf16_at(vr[u][r], vscale[u][r], i / 2);
+                a0[2 * u] = __builtin_amdgcn_perm(w[1], w[0], 0x05040100u);
+                a1[2 * u] = __builtin_amdgcn_perm(w[1], w[0], 0x07060302u);
+                a0[2 * u + 1] = __builtin_amdgcn_perm(w[3], w[2], 0x05040100u);
+                a1[2 * u + 1] = __builtin_amdgcn_perm(w[3], w[2], 0x07060302u);
+            } else if constexpr (KV == kE4m3) {
                 // Bytes (row a, row b) of elements i and i + 1, then one widening per element.
                 const int c = i / 4;
                 const uint32_t sel = (i % 4) == 0 ? 0x05010400u : 0x07030602u;
@@ -830,11 +931,13 @@ __device__ __forceinline__ void scan_sequences(const SplitParams &p, int32_t *s_
 // Declared here, keyed only on the tile shape, so that a kernel running the
 // worker in several modes (prefix sharing: own and shared pages in different
 // workgroups) holds one such array, not one per mode.
-template <int D, bool FP8>
+template <int D, int KV>
 __device__ __forceinline__ uint8_t *k_regroup_stage()
 {
+    if constexpr (KV == kFp4)
+        return nullptr;   // nothing is regrouped
     __shared__ __attribute__((aligned(16)))
-    uint8_t k_stage[kWavesPerBlock][kPageSize * D * (FP8 ? 1 : 2)];
+    uint8_t k_stage[kWavesPerBlock][kPageSize * D * (KV == kE4m3 ? 1 : 2)];
     return k_stage[__builtin_amdgcn_readfirstlane(threadIdx.x / kWave)];
 }
 
@@ -861,7 +964,7 @@ struct StreamLds {
 // complete: the caller has passed a barrier). A worker is one wavefront, or
 // for kSharedPages the four wavefronts of a workgroup, which stream the same
 // tiles and compute column blocks blk = 0..3 of each shared unit.
-template <int D, bool FP8, int MODE>
+template <int D, int KV, int MODE>
 __device__ __forceinline__ void split_unit_worker(const SplitParams &p, int w, const StreamLds &sv, int blk = -1)
 {
     constexpr bool kShared = MODE == kSharedPages;
@@ -869,10 +972,10 @@ __device__ __forceinline__ void split_unit_worker(const SplitParams &p, int w, c
     if (w >= p.num_workers)
         return;
     const int nseq = kShared ? sv.num_groups : p.batch;   // "sequences" of the stream
-    constexpr int NT = step_tiles<D, FP8>();
+    constexpr int NT = step_tiles<D, KV>();
     const int Hkv = p.num_kv_heads;
     const long long total = (long long)sv.cum[nseq] * Hkv;
-    const int nw = effective_workers(total, p.num_workers, NT, kShared ? 0 : wide_from(p.num_workers, FP8));
+    const int nw = effective_workers(total, p.num_workers, NT, kShared ? 0 : wide_from(p.num_workers, KV));
     if (w >= nw)
         return;
     const int s0 = __builtin_amdgcn_readfirstlane((int)((long long)w * total / nw));
@@ -883,7 +986,7 @@ __device__ __forceinline__ void split_unit_worker(const SplitParams &p, int w, c
     const int n = lane & 15;
     const int quad = lane >> 4;
     const int G = p.group;
-    uint8_t *lds = k_regroup_stage<D, FP8>();
+    uint8_t *lds = k_regroup_stage<D, KV>();
     // Plain attention: a per-wave stage (see stage_output) holding the
     // partial state of the range's first piece, if cut (G * (D + 2) fp32 at
     // the start), then the output rows of finished units, `staged` of them
@@ -980,18 +1083,18 @@ __device__ __forceinline__ void split_unit_worker(const SplitParams &p, int w, c
     int cpos = 0, cnext = kChunk;   // lane of the next step to issue; first step of the chunk in `ahead`
     Desc ahead = find(0);
     settle(ahead);
-    auto issue = [&](Step<D, FP8, NT> &x, int i, bool with_q) {   // step i of the range, from lane cpos
+    auto issue = [&](Step<D, KV, NT> &x, int i, bool with_q) {   // step i of the range, from lane cpos
         int32_t T[NT];
 #pragma unroll
         for (int u = 0; u < NT; ++u)
             T[u] = __builtin_amdgcn_readlane(tile[u], cpos);
         x.meta = (uint32_t)__builtin_amdgcn_readlane((int)lmeta, cpos);
         x.valid = __builtin_amdgcn_readlane(lvalid, cpos);
-        issue_step<D, FP8, NT, !kShared>(x, p, T, i < nsteps, with_q || (x.meta & kMetaFirst) != 0, n, quad, lane, blk);
+        issue_step<D, KV, NT, !kShared>(x, p, T, i < nsteps, with_q || (x.meta & kMetaFirst) != 0, n, quad, lane, blk);
         ++cpos;
     };
 
-    Step<D, FP8, NT> buf[kNbuf];
+    Step<D, KV, NT> buf[kNbuf];
 #pragma unroll
     for (int k = 0; k < kNbuf - 1; ++k)
         issue(buf[k], k, k == 0);
@@ -1018,7 +1121,7 @@ __device__ __forceinline__ void split_unit_worker(const SplitParams &p, int w, c
             }
             issue(buf[(k + kNbuf - 1) % kNbuf], i + kNbuf - 1, false);
             if (i < nsteps) {
-                const Step<D, FP8, NT> &t = buf[k];
+                const Step<D, KV, NT> &t = buf[k];
                 const uint32_t meta = t.meta;
                 const bool ends = i == nsteps - 1;
                 if (i == 0 || (meta & kMetaFirst) != 0) {
@@ -1038,13 +1141,13 @@ __device__ __forceinline__ void split_unit_worker(const SplitParams &p, int w, c
                 constexpr bool kFew = NT == 4 && !kShared;
                 const int valid = kShared ? t.valid & 0xff : t.valid;
                 if (kFew && (meta & kMetaLast) == 0)
-                    compute_step<D, FP8, NT>(st, t.t, qop, p.scale_log2, kPageSize * NT, lds, lane, n, quad);
+                    compute_step<D, KV, NT>(st, t.t, qop, p.scale_log2, kPageSize * NT, lds, lane, n, quad);
                 else if (kFew && valid <= kPageSize)
-                    compute_step<D, FP8, 1>(st, t.t, qop, p.scale_log2, valid, lds, lane, n, quad);
+                    compute_step<D, KV, 1>(st, t.t, qop, p.scale_log2, valid, lds, lane, n, quad);
                 else if (kFew && valid <= 2 * kPageSize)
-                    compute_step<D, FP8, 2>(st, t.t, qop, p.scale_log2, valid, lds, lane, n, quad);
+                    compute_step<D, KV, 2>(st, t.t, qop, p.scale_log2, valid, lds, lane, n, quad);
                 else
-                    compute_step<D, FP8, NT>(st, t.t, qop, p.scale_log2, valid, lds, lane, n, quad);
+                    compute_step<D, KV, NT>(st, t.t, qop, p.scale_log2, valid, lds, lane, n, quad);
                 if (kShared && ((meta & kMetaLast) != 0 || ends)) {
                     // A shared unit's state is always merged: a whole one goes to the unit area
                     // (indexed by first query row / G), a cut one to the worker's slot; block blk

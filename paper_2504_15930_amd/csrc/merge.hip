@@ -189,7 +189,7 @@ __global__ __launch_bounds__(kMergeThreads) void merge_kernel(MergeParams p)
             *reinterpret_cast<u32x2_t *>(dst) = u32x2_t{fill, fill};
         return;
     }
-    const int NW = effective_workers(total, p.num_workers, p.step_tiles, wide_from(p.num_workers, p.fp8 != 0));
+    const int NW = effective_workers(total, p.num_workers, p.step_tiles, wide_from(p.num_workers, p.kv));
     const long long a = (long long)Hkv * cb + (long long)g * nb;   // first step of the unit
     const Cut cut = cuts_of(a, nb, total, NW, a, nb, total, NW, lane).s;
     if (cut.pieces == 1)
@@ -245,10 +245,10 @@ __global__ __launch_bounds__(kMergeThreads) void merge_prefix_kernel(PrefixMerge
             *reinterpret_cast<u32x2_t *>(dst) = u32x2_t{fill, fill};
         return;
     }
-    const int nw_o = effective_workers(tot_o, p.num_workers, p.step_tiles, wide_from(p.num_workers, p.fp8 != 0));
+    const int nw_o = effective_workers(tot_o, p.num_workers, p.step_tiles, wide_from(p.num_workers, p.kv));
     const int nw_s = effective_workers(tot_s,
                                        effective_shared_workers(tot_o, p.num_workers, p.num_shared_workers,
-                                                                p.max_shared_workers, p.step_tiles, p.fp8 != 0),
+                                                                p.max_shared_workers, p.step_tiles, p.kv),
                                        p.step_tiles, 0);
     const long long a_o = (long long)Hkv * co + (long long)g * ob;
     const long long a_s = (long long)Hkv * s_start + (long long)g * ss;
@@ -293,7 +293,7 @@ hipError_t launch_merge(const MergeParams &p, int head_dim, hipStream_t stream)
 {
     const int per_block = kMergeThreads / kWave;
     static_assert(kMergeThreads == kAppendThreads, "the append's workgroups ride in the merge's launch");
-    const AppendKind kind = p.has_next ? append_kind(p.next, p.fp8 != 0) : kNoAppend;
+    const AppendKind kind = p.has_next ? append_kind(p.next, p.kv == kE4m3) : kNoAppend;
     const long long next_blocks = p.has_next ? append_blocks(p.next, kind) : 0;
     // A grid has at most 65535 rows; with few heads and thousands of sequences
     // the append's workgroups take wider ones (the merge's beyond the heads exit).

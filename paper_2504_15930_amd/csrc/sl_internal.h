@@ -43,6 +43,10 @@
 namespace sl {
 
 constexpr int kPageSize = 16;
+// What a cache's pages hold: bf16 rows, E4M3 codes with a scale per page-head
+// tile, or the records of fp4_unit.h (E2M1 codes with a scale per 32 elements).
+enum Kv : int { kBf16 = 0, kE4m3 = 1, kFp4 = 2 };
+constexpr size_t fp4_record_bytes(int head_dim) { return 17 * (size_t)head_dim; }
 constexpr int kWave = 64;
 constexpr int kWavesPerBlock = 4;          // split kernel: 4 independent workers per block
 constexpr int kMaxGroup = 16;              // query heads per KV head (one MFMA column block)
@@ -82,7 +86,7 @@ __host__ __device__ inline int effective_workers(long long total, int num_worker
 }
 // `wide` for plain attention's stream and the own pages of prefix sharing; the
 // shared pages' is 0.
-__host__ __device__ inline int wide_from(int num_workers, bool fp8) { return fp8 ? num_workers / 2 : num_workers; }
+__host__ __device__ inline int wide_from(int num_workers, int kv) { return kv != kBf16 ? num_workers / 2 : num_workers; }
 // Prefix sharing: shared-page workgroups that take part in a call. The launch
 // holds the own-page workgroups and up to twice `base` shared ones, and a CU
 // holds two such workgroups; own-page workgroups without work exit at once,
@@ -96,12 +100,12 @@ __host__ __device__ inline int wide_from(int num_workers, bool fp8) { return fp8
 //   32 of 4000 x 16, 16/1 heads                                    480  76 us, 256  83
 // The split kernel and the merge derive it from the same totals (own tiles).
 __host__ __device__ inline int effective_shared_workers(long long own_total, int own_workers, int base,
-                                                        int max_workers, int step_tiles, bool fp8)
+                                                        int max_workers, int step_tiles, int kv)
 {
     const int own_blocks = (own_workers + kWavesPerBlock - 1) / kWavesPerBlock;
     const int active =
         own_total > 0
-            ? (effective_workers(own_total, own_workers, step_tiles, wide_from(own_workers, fp8)) + kWavesPerBlock - 1) /
+            ? (effective_workers(own_total, own_workers, step_tiles, wide_from(own_workers, kv)) + kWavesPerBlock - 1) /
                   kWavesPerBlock
             : 0;
     const int idle = own_blocks - active;
@@ -142,7 +146,7 @@ struct Workspace {
 
 struct SplitParams {
     const uint16_t *q;
-    const void *k_pages;
+    const void *k_pages;   // FP4: the records, which hold K, V and scales
     const void *v_pages;
     const float *k_scales;
     const float *v_scales;
@@ -214,7 +218,7 @@ struct PrefixMergeParams {
     int32_t num_shared_workers;   // base and largest count of shared-page workgroups
     int32_t max_shared_workers;   // (effective_shared_workers)
     int32_t step_tiles;           // as the split kernel's
-    int32_t fp8;
+    int32_t kv;                   // Kv of the cache
     uint32_t group_inverse;       // ceil(2^32 / group), for heads below 2^28 (unused for a group of 1)
 };
 
@@ -248,7 +252,7 @@ struct MergeParams {
     uint16_t *out;
     int32_t batch, num_q_heads, num_kv_heads, group, num_workers;
     int32_t step_tiles;   // as the split kernel's
-    int32_t fp8;
+    int32_t kv;           // Kv of the cache
     uint32_t group_inverse;   // as PrefixMergeParams'
     // Decode engine: the next step's staged append (and its bookkeeping) runs
     // in the same launch, in workgroups after the merge's, if has_next is set.
@@ -284,23 +288,49 @@ inline size_t prefix_dynamic_lds(int batch, int max_sub)
 {
     return sizeof(int32_t) * (3 * (size_t)batch + 2 * (size_t)max_sub + 3);
 }
-hipError_t launch_split(const SplitParams &p, int head_dim, bool fp8, hipStream_t stream);
+using SplitKernel = void (*)(SplitParams);
+using PrefixKernel = void (*)(SplitParams, SplitParams, PrefixParams, int, int);
+SplitKernel split_fp4_kernel_of(int head_dim);     // decode_fp4.hip (null: no such head_dim)
+PrefixKernel prefix_fp4_kernel_of(int head_dim);
+hipError_t launch_split(const SplitParams &p, int head_dim, int kv, hipStream_t stream);
 // Prefix mode: the own-page pass (single-unit workers) and the shared-page
 // pass (one workgroup of kPrefixBlocks wavefronts per worker, one 16-row
 // column block each, partial states only) in one launch, followed by the
 // merge. shared.num_workers is the base count of shared workgroups and
 // max_shared the largest (effective_shared_workers).
 hipError_t launch_prefix_split(const SplitParams &own, const SplitParams &shared, int max_shared,
-                               const PrefixParams &pp, int head_dim, bool fp8, hipStream_t stream);
+                               const PrefixParams &pp, int head_dim, int kv, hipStream_t stream);
 hipError_t launch_merge_prefix(const PrefixMergeParams &p, int head_dim, hipStream_t stream);
 hipError_t launch_merge(const MergeParams &p, int head_dim, hipStream_t stream);
 hipError_t launch_append(const AppendParams &p, int head_dim, bool fp8, hipStream_t stream);
+// Rows of the 4-bit cache (fp4_rows.hip): k_rows / v_rows [rows][Hkv][D] into
+// it, or from it to k_out / v_out where k_rows is null. Row t's slot is
+// slots[t] (page * 16 + slot in the page), or, with slots null, that of token
+// seq_lens[t] - 1 of sequence t through the block table.
+struct Fp4RowParams {
+    const uint16_t *k_rows, *v_rows;
+    uint16_t *k_out, *v_out;
+    const int32_t *slots, *block_table, *seq_lens;
+    uint8_t *pages;   // [num_pages][Hkv][17 D]
+    int32_t rows, num_kv_heads, max_blocks, num_pages;
+};
+hipError_t launch_fp4_rows(const Fp4RowParams &p, int head_dim, hipStream_t stream);
+// Page bookkeeping (pages.hip).
+struct PageParams {
+    const int32_t *seq_lens, *new_tokens, *finished;
+    int32_t *block_table, *free_pages;
+    const int32_t *free_count;
+    int32_t *seq_lens_out, *free_count_out, *token_start, *slots;
+    int32_t batch, max_blocks, num_pages, max_tokens;
+};
+hipError_t launch_extend_pages(const PageParams &p, hipStream_t stream);
+hipError_t launch_release_pages(const PageParams &p, hipStream_t stream);
 // Decode engine helper (engine.hip): fill prompt pages with synthetic data.
 hipError_t launch_engine_fill(const int32_t *pages, int n_pages, int hkv, int head_dim, bool fp8, uint32_t seed,
                               void *k_pages, void *v_pages, float *k_scales, float *v_scales, hipStream_t stream);
 // Pages per pipeline step of the split kernels (their streams are counted in steps).
-int split_step_tiles(int head_dim, bool fp8);
+int split_step_tiles(int head_dim, int kv);
 // Resident split-kernel workgroups per CU (occupancy query), for the default worker count.
-hipError_t split_blocks_per_cu(int head_dim, bool fp8, int *blocks);
+hipError_t split_blocks_per_cu(int head_dim, int kv, int *blocks);
 
 }  // namespace sl

@@ -18,13 +18,15 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 # SL_LIBRARY may name another build of the same sources (the host-sanitized one of the tests).
 LIBRARY = os.environ.get("SL_LIBRARY") or os.path.join(HERE, "libsl.so")
 
+PAGE_SIZE = 16
 SL_OK = 0
 STATUS_NAMES = {0: "SL_OK", -1: "SL_ERR_NULL", -2: "SL_ERR_SHAPE", -3: "SL_ERR_UNSUPPORTED",
                 -4: "SL_ERR_WORKSPACE", -5: "SL_ERR_HIP", -6: "SL_ERR_ALIGNMENT", -7: "SL_ERR_SCRATCH_LIMIT"}
 EXPORTS = ["sl_decode_attn_workspace_size", "sl_decode_attn_num_workers", "sl_decode_attn",
            "sl_decode_attn_fp8", "sl_kv_append", "sl_kv_append_fp8", "sl_decode_attn_prefix",
            "sl_decode_attn_prefix_fp8", "sl_decode_attn_prefix_workspace_size", "sl_decode_attn_noalloc",
-           "sl_status_string"]
+           "sl_decode_attn_fp4", "sl_decode_attn_prefix_fp4", "sl_kv_append_fp4", "sl_kv_write_fp4", "sl_kv_read_fp4",
+           "sl_pages_extend", "sl_pages_release", "sl_status_string"]
 # include/sl_engine.h (typed in engine.py)
 ENGINE_EXPORTS = ["sl_engine_create", "sl_engine_run", "sl_engine_schedule", "sl_engine_destroy"]
 # include/sl_dispatch.h (typed in dispatch.py)
@@ -82,6 +84,13 @@ def load(path: str = LIBRARY) -> ctypes.CDLL:
     lib.sl_decode_attn_prefix_workspace_size.argtypes = [D, ctypes.c_int32, ctypes.POINTER(ctypes.c_size_t)]
     lib.sl_kv_append_fp8.argtypes = [D, P, P, P, P, P, P, P, P]
     lib.sl_decode_attn_noalloc.argtypes = [D, P, P, P, P, P, ctypes.c_float, P]
+    lib.sl_decode_attn_fp4.argtypes = [D, P, P, P, P, ctypes.c_float, P]
+    lib.sl_decode_attn_prefix_fp4.argtypes = [D, P, P, P, P, P, P, ctypes.c_int32, ctypes.c_float, P]
+    lib.sl_kv_append_fp4.argtypes = [D, P, P, P, P, P]
+    lib.sl_kv_write_fp4.argtypes = [D, P, P, P, ctypes.c_int32, P]
+    lib.sl_kv_read_fp4.argtypes = [D, P, P, ctypes.c_int32, P, P]
+    lib.sl_pages_extend.argtypes = [D, P, P, P, P, P, ctypes.c_int32, P, P, P, P]
+    lib.sl_pages_release.argtypes = [D, P, P, P, P, P, P, P]
     lib.sl_status_string.argtypes = [ctypes.c_int32]
     lib.sl_status_string.restype = ctypes.c_char_p
     for name in EXPORTS[:-1]:
@@ -421,3 +430,205 @@ def decode_attn_prefix_fp8(q, k_pages, v_pages, k_scales, v_scales, block_table,
     """``sl_decode_attn_prefix_fp8``: prefix sharing over uint8 E4M3 pages with fp32 [N, Hkv] scales."""
     return _run_prefix(True, q, k_pages, v_pages, k_scales, v_scales, block_table, seq_lens, scale, group_start,
                        shared_pages, out, num_workers, workspace, timing)
+
+
+# The 4-bit cache: one uint8 record of 17 D bytes per (page, KV head), as include/sl.h lays it out.
+FP4_BLOCK = 32   # elements per scale
+
+
+def fp4_record_bytes(head_dim: int) -> int:
+    """Bytes of a page-head record of the 4-bit cache (16 tokens, keys and values)."""
+    return 17 * head_dim
+
+
+def _need_on(index: int, t: torch.Tensor, name: str, dtype, shape):
+    """``t`` of this dtype and exact shape, contiguous, on GPU ``index``."""
+    _need(t, name, dtype, len(shape))
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.get_device() != index:
+        raise ValueError(f"{name} must be on cuda:{index} with the others")
+
+
+def _fp4_pool(kv_pages, head_dim: int) -> tuple[int, int, int]:
+    """(GPU, num_pages, num_kv_heads) of a pool for rows of ``head_dim`` elements."""
+    _need(kv_pages, "kv_pages", torch.uint8, 3)
+    if kv_pages.shape[2] != 17 * head_dim:
+        raise ValueError(f"kv_pages must hold records of {17 * head_dim} bytes for head_dim {head_dim}, "
+                         f"got {kv_pages.shape[2]}")
+    return kv_pages.get_device(), kv_pages.shape[0], kv_pages.shape[1]
+
+
+def _run_fp4(q, kv_pages, block_table, seq_lens, scale, groups, out, num_workers, workspace, timing):
+    _need(q, "q", torch.bfloat16, 3)
+    B, Hq, D = q.shape
+    index, N, Hkv = _fp4_pool(kv_pages, D)
+    _need_on(index, q, "q", torch.bfloat16, q.shape)
+    _need(block_table, "block_table", torch.int32, 2)
+    _need_on(index, block_table, "block_table", torch.int32, (B, block_table.shape[1]))
+    _need_on(index, seq_lens, "seq_lens", torch.int32, (B,))
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _need_on(index, out, "out", torch.bfloat16, q.shape)
+    if groups is not None:
+        group_start, shared_pages = groups
+        _need(shared_pages, "shared_pages", torch.int32, 1)
+        ng = shared_pages.shape[0]
+        _need_on(index, shared_pages, "shared_pages", torch.int32, (ng,))
+        _need_on(index, group_start, "group_start", torch.int32, (ng + 1,))
+    with _device(index):
+        stream = _stream(index)
+        sizes = (B, Hq, Hkv, D, PAGE_SIZE, block_table.shape[1], N, num_workers)
+        desc = make_desc(*sizes, stream)
+        if B == 0:
+            return out
+        if workspace is None:
+            workspace = _workspace(index, stream, _workspace_bytes(index, *sizes) if groups is None else
+                                   _prefix_workspace_bytes(index, ng, *sizes))
+        desc.workspace = workspace.data_ptr()
+        desc.workspace_bytes = workspace.numel() * workspace.element_size()
+        if timing is not None:
+            desc.timing_start, desc.timing_stop = timing
+        lib = load()
+        if groups is None:
+            _check(lib.sl_decode_attn_fp4(ctypes.byref(desc), q.data_ptr(), kv_pages.data_ptr(),
+                                          block_table.data_ptr(), seq_lens.data_ptr(), float(scale), out.data_ptr()),
+                   "sl_decode_attn_fp4")
+        else:
+            _check(lib.sl_decode_attn_prefix_fp4(ctypes.byref(desc), q.data_ptr(), kv_pages.data_ptr(),
+                                                 block_table.data_ptr(), seq_lens.data_ptr(), group_start.data_ptr(),
+                                                 shared_pages.data_ptr(), ng, float(scale), out.data_ptr()),
+                   "sl_decode_attn_prefix_fp4")
+    return out
+
+
+def decode_attn_fp4(q, kv_pages, block_table, seq_lens, scale, *, out=None, num_workers=0, workspace=None,
+                    timing=None) -> torch.Tensor:
+    """``sl_decode_attn_fp4``: decode attention over a 4-bit cache, ``kv_pages`` uint8
+    [num_pages, Hkv, ``fp4_record_bytes(D)``]; otherwise as ``decode_attn``."""
+    return _run_fp4(q, kv_pages, block_table, seq_lens, scale, None, out, num_workers, workspace, timing)
+
+
+def decode_attn_prefix_fp4(q, kv_pages, block_table, seq_lens, scale, group_start, shared_pages, *, out=None,
+                           num_workers=0, workspace=None, timing=None) -> torch.Tensor:
+    """``sl_decode_attn_prefix_fp4``: prefix sharing over a 4-bit cache; groups as ``decode_attn_prefix``."""
+    return _run_fp4(q, kv_pages, block_table, seq_lens, scale, (group_start, shared_pages), out, num_workers,
+                    workspace, timing)
+
+
+def kv_append_fp4(k_new, v_new, block_table, seq_lens, kv_pages, *, timing=None):
+    """``sl_kv_append_fp4``: a decode step's new rows [B, Hkv, D] (bf16) quantised into a 4-bit cache, in place;
+    ``seq_lens`` already counts them. Asynchronous on the current stream."""
+    _need(k_new, "k_new", torch.bfloat16, 3)
+    B, Hkv, D = k_new.shape
+    index, N, heads = _fp4_pool(kv_pages, D)
+    _need_on(index, k_new, "k_new", torch.bfloat16, (B, heads, D))
+    _need_on(index, v_new, "v_new", torch.bfloat16, (B, heads, D))
+    _need(block_table, "block_table", torch.int32, 2)
+    _need_on(index, block_table, "block_table", torch.int32, (B, block_table.shape[1]))
+    _need_on(index, seq_lens, "seq_lens", torch.int32, (B,))
+    with _device(index):
+        desc = make_desc(B, Hkv, Hkv, D, PAGE_SIZE, block_table.shape[1], N, 0, _stream(index), timing=timing)
+        _check(load().sl_kv_append_fp4(ctypes.byref(desc), k_new.data_ptr(), v_new.data_ptr(),
+                                       block_table.data_ptr(), seq_lens.data_ptr(), kv_pages.data_ptr()),
+               "sl_kv_append_fp4")
+
+
+def kv_write_fp4(k_new, v_new, slots, kv_pages, *, timing=None):
+    """``sl_kv_write_fp4``: rows [T, Hkv, D] (bf16) quantised into the slots ``slots`` (int32 [T], page * 16 + slot in
+    the page; negative: no token) of a 4-bit cache, in place. Asynchronous on the current stream."""
+    _need(k_new, "k_new", torch.bfloat16, 3)
+    T, Hkv, D = k_new.shape
+    index, N, heads = _fp4_pool(kv_pages, D)
+    _need_on(index, k_new, "k_new", torch.bfloat16, (T, heads, D))
+    _need_on(index, v_new, "v_new", torch.bfloat16, (T, heads, D))
+    _need_on(index, slots, "slots", torch.int32, (T,))
+    with _device(index):
+        desc = make_desc(0, Hkv, Hkv, D, PAGE_SIZE, 1, N, 0, _stream(index), timing=timing)
+        _check(load().sl_kv_write_fp4(ctypes.byref(desc), k_new.data_ptr(), v_new.data_ptr(), slots.data_ptr(), T,
+                                      kv_pages.data_ptr()), "sl_kv_write_fp4")
+
+
+def kv_read_fp4(slots, kv_pages, *, k_out=None, v_out=None, timing=None) -> tuple[torch.Tensor, torch.Tensor]:
+    """``sl_kv_read_fp4``: the key and value rows (bf16 [T, Hkv, D]) in the slots ``slots`` (int32 [T]) of a 4-bit
+    cache; zero rows for negative slots, NaN for slots past the pool. Asynchronous on the current stream."""
+    _need(kv_pages, "kv_pages", torch.uint8, 3)
+    if kv_pages.shape[2] % 17:
+        raise ValueError(f"kv_pages must hold records of 17 D bytes, got {kv_pages.shape[2]}")
+    D = kv_pages.shape[2] // 17
+    index, N, Hkv = _fp4_pool(kv_pages, D)
+    _need(slots, "slots", torch.int32, 1)
+    T = slots.shape[0]
+    _need_on(index, slots, "slots", torch.int32, (T,))
+    rows = []
+    for t, name in ((k_out, "k_out"), (v_out, "v_out")):
+        if t is None:
+            t = torch.empty((T, Hkv, D), dtype=torch.bfloat16, device=kv_pages.device)
+        else:
+            _need_on(index, t, name, torch.bfloat16, (T, Hkv, D))
+        rows.append(t)
+    with _device(index):
+        desc = make_desc(0, Hkv, Hkv, D, PAGE_SIZE, 1, N, 0, _stream(index), timing=timing)
+        _check(load().sl_kv_read_fp4(ctypes.byref(desc), kv_pages.data_ptr(), slots.data_ptr(), T,
+                                     rows[0].data_ptr(), rows[1].data_ptr()), "sl_kv_read_fp4")
+    return rows[0], rows[1]
+
+
+def _pages_args(seq_lens, marks, marks_name, block_table, free_pages, free_count, seq_lens_out, free_count_out):
+    """Checks common to the page bookkeeping; returns (GPU, batch, max_blocks, num_pages, the two outputs)."""
+    _need(seq_lens, "seq_lens", torch.int32, 1)
+    _need(block_table, "block_table", torch.int32, 2)
+    _need(free_pages, "free_pages", torch.int32, 1)
+    index, B, blocks, N = seq_lens.get_device(), seq_lens.shape[0], block_table.shape[1], free_pages.shape[0]
+    _need_on(index, marks, marks_name, torch.int32, (B,))
+    _need_on(index, block_table, "block_table", torch.int32, (B, blocks))
+    _need_on(index, free_pages, "free_pages", torch.int32, (N,))
+    _need_on(index, free_count, "free_count", torch.int32, (1,))
+    outs = []
+    for t, name, like in ((seq_lens_out, "seq_lens_out", seq_lens), (free_count_out, "free_count_out", free_count)):
+        if t is None:
+            t = torch.empty_like(like)
+        else:
+            _need_on(index, t, name, torch.int32, like.shape)
+        outs.append(t)
+    return index, B, blocks, N, outs
+
+
+def pages_extend(seq_lens, new_tokens, block_table, free_pages, free_count, max_tokens, *, seq_lens_out=None,
+                 free_count_out=None, token_start=None, slots=None):
+    """``sl_pages_extend``: room for ``new_tokens`` [B] more tokens per request. Pages come from the top of the stack
+    ``free_pages`` [num_pages] (the first ``free_count`` [1] of it are free) and are entered in ``block_table``, in
+    place. Returns ``(seq_lens_out, token_start, slots, free_count_out)``: the new lengths [B], where each request's
+    tokens begin in the slot map [B + 1], the slot map [max_tokens] (-1 past the last token), and the pages left.
+    ``seq_lens_out`` and ``free_count_out`` may be the inputs themselves. All int32; asynchronous."""
+    index, B, blocks, N, (lens, count) = _pages_args(seq_lens, new_tokens, "new_tokens", block_table, free_pages,
+                                                     free_count, seq_lens_out, free_count_out)
+    if token_start is None:
+        token_start = torch.empty(B + 1, dtype=torch.int32, device=seq_lens.device)
+    else:
+        _need_on(index, token_start, "token_start", torch.int32, (B + 1,))
+    if slots is None:
+        slots = torch.empty(max_tokens, dtype=torch.int32, device=seq_lens.device)
+    else:
+        _need_on(index, slots, "slots", torch.int32, (max_tokens,))
+    with _device(index):
+        desc = make_desc(B, 1, 1, 64, PAGE_SIZE, blocks, N, 0, _stream(index))
+        _check(load().sl_pages_extend(ctypes.byref(desc), seq_lens.data_ptr(), new_tokens.data_ptr(),
+                                      block_table.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(),
+                                      max_tokens, lens.data_ptr(), count.data_ptr(), token_start.data_ptr(),
+                                      slots.data_ptr()), "sl_pages_extend")
+    return lens, token_start, slots, count
+
+
+def pages_release(finished, seq_lens, block_table, free_pages, free_count, *, seq_lens_out=None, free_count_out=None):
+    """``sl_pages_release``: the pages of requests with ``finished`` [B] not 0 go back on the stack, in place, and
+    their lengths become 0. Returns ``(seq_lens_out, free_count_out)``, which may be the inputs themselves."""
+    index, B, blocks, N, (lens, count) = _pages_args(seq_lens, finished, "finished", block_table, free_pages,
+                                                     free_count, seq_lens_out, free_count_out)
+    with _device(index):
+        desc = make_desc(B, 1, 1, 64, PAGE_SIZE, blocks, N, 0, _stream(index))
+        _check(load().sl_pages_release(ctypes.byref(desc), finished.data_ptr(), seq_lens.data_ptr(),
+                                       block_table.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(),
+                                       lens.data_ptr(), count.data_ptr()), "sl_pages_release")
+    return lens, count
