@@ -87,8 +87,9 @@ typedef struct sl_attn_desc {
     int32_t max_blocks_per_seq; /* row length of block_table */
     int32_t num_pages;          /* pages in each pool; valid page ids are [0, num_pages) */
     int32_t num_workers;        /* split-KV workers (wavefronts). 0: library default
-                                   (three per CU for a bf16 cache with head_dim 128, else,
-                                   and for prefix-shared attention, four per CU);
+                                   (three per CU for a bf16 cache with head_dim 128, eight
+                                   for a 4-bit one with head_dim 64, else, and for
+                                   prefix-shared attention, four per CU);
                                    1..65536: exactly this many. The result does not depend on it beyond fp32
                                    rounding; tests vary it to exercise the merge. */
     hipStream_t stream;         /* stream the work is enqueued on (0: null stream) */
@@ -100,8 +101,8 @@ typedef struct sl_attn_desc {
 } sl_attn_desc;
 
 /*
- * Bytes of workspace the calls need for `desc` (sizes and num_workers; no
- * pointer is read). With num_workers == 0 this queries the current device.
+ * Bytes of workspace the calls need for `desc`, whichever the cache (sizes and
+ * num_workers; no pointer is read). With num_workers == 0 this queries the current device.
  * Errors: SL_ERR_NULL, SL_ERR_SHAPE, SL_ERR_UNSUPPORTED, SL_ERR_HIP.
  */
 sl_status sl_decode_attn_workspace_size(const sl_attn_desc *desc, size_t *bytes);
@@ -199,8 +200,8 @@ sl_status sl_decode_attn_prefix_fp8(const sl_attn_desc *desc, const uint16_t *q,
                                     const int32_t *group_start, const int32_t *shared_pages,
                                     int32_t num_groups, float scale, uint16_t *out);
 
-/* Workspace bytes sl_decode_attn_prefix and sl_decode_attn_prefix_fp8 need
- * for desc and num_groups (one size serves both). */
+/* Workspace bytes sl_decode_attn_prefix, sl_decode_attn_prefix_fp8 and
+ * sl_decode_attn_prefix_fp4 need for desc and num_groups (one size serves all). */
 sl_status sl_decode_attn_prefix_workspace_size(const sl_attn_desc *desc, int32_t num_groups,
                                                size_t *bytes);
 

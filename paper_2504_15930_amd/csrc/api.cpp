@@ -141,10 +141,17 @@ sl_status resolve_workers(const sl_attn_desc *d, int kv, int *nw, bool prefix = 
     // one per CU is as fast or faster (384 sequences of 1..2048 tokens: 130 us,
     // with three per four CUs 132; with one tile per step 132 and 150). Two waves per SIMD
     // were slower for all but E4M3 with head_dim 64 and one tile per step.
+    // A 4-bit cache with head_dim 64 takes two per CU: its tiles are so short that
+    // instructions set the pace, and one wavefront's fill the other's waits (384
+    // sequences of 1..2048 tokens, 32/8 heads: 51.6 us, with one 59.4). With head_dim
+    // 128 two were slower (512 x 512 + lognormal(2048), 28/4 heads: 173 us with one,
+    // 188 with two; 256 of 64/8 heads 350 and 368).
     // Prefix-shared attention keeps one own-page workgroup per CU beside its shared-page
     // workgroups (three per four CUs was 12% slower).
     const int blocks = info->blocks[d->head_dim == 128][kv];
-    const int per_cu4 = kv != kBf16 || prefix || d->head_dim == 64 ? 4 : 3;   // workgroups per four CUs
+    const int per_cu4 = kv == kFp4 && !prefix && d->head_dim == 64 && blocks > 1 ? 8   // workgroups per four CUs
+                        : kv != kBf16 || prefix || d->head_dim == 64             ? 4
+                                                                                 : 3;
     *nw = (blocks > 0 ? info->cus * per_cu4 / 4 : info->cus) * kWavesPerBlock;
     if (*nw > kMaxWorkers)
         *nw = kMaxWorkers;
@@ -235,7 +242,7 @@ sl_status run(const sl_attn_desc *d, const uint16_t *q, const void *k_pages, con
     mp.num_kv_heads = d->num_kv_heads;
     mp.group = G;
     mp.num_workers = nw;
-    mp.step_tiles = split_step_tiles(d->head_dim, kv);
+    mp.step_tiles = split_step_tiles(d->head_dim, kv, false);
     mp.group_inverse = inverse_of(G);
     mp.kv = kv;
     mp.has_next = next != nullptr;
@@ -411,7 +418,7 @@ sl_status run_prefix(const sl_attn_desc *d, const uint16_t *q, const void *k_pag
     mp.num_shared_workers = nws;
     mp.max_shared_workers = nws_max;
     mp.max_blocks = d->max_blocks_per_seq;
-    mp.step_tiles = split_step_tiles(d->head_dim, kv);
+    mp.step_tiles = split_step_tiles(d->head_dim, kv, true);
     mp.group_inverse = inverse_of(G);
     mp.kv = kv;
     if (launch_merge_prefix(mp, d->head_dim, d->stream) != hipSuccess)
@@ -539,14 +546,15 @@ sl_status sl_decode_attn_workspace_size(const sl_attn_desc *desc, size_t *bytes)
         return st;
     if (!bytes)
         return SL_ERR_NULL;
-    // Size for the larger of the bf16 and fp8 worker counts, so one workspace serves both.
-    int nw_bf16 = 0, nw_fp8 = 0;
-    st = sl::resolve_workers(desc, false, &nw_bf16);
-    if (st == SL_OK)
-        st = sl::resolve_workers(desc, true, &nw_fp8);
-    if (st != SL_OK)
-        return st;
-    const int nw = nw_bf16 > nw_fp8 ? nw_bf16 : nw_fp8;
+    // Sized for the largest of the three caches' worker counts, so one workspace serves them all.
+    int nw = 0;
+    for (int kv = sl::kBf16; kv <= sl::kFp4; ++kv) {
+        int n = 0;
+        st = sl::resolve_workers(desc, kv, &n);
+        if (st != SL_OK)
+            return st;
+        nw = n > nw ? n : nw;
+    }
     *bytes = sl::workspace_layout(nullptr, desc->batch, desc->max_blocks_per_seq,
                                   desc->num_kv_heads, desc->num_q_heads / desc->num_kv_heads,
                                   desc->head_dim, nw, nullptr);
@@ -596,16 +604,15 @@ sl_status sl_decode_attn_prefix_workspace_size(const sl_attn_desc *desc, int32_t
         return st;
     if (!bytes)
         return SL_ERR_NULL;
-    // Sized for the larger of the bf16 and E4M3 worker counts, so one
-    // workspace serves both entry points.
-    int nw = 0, nw_fp8 = 0;
-    st = sl::resolve_workers(desc, false, &nw, true);
-    if (st == SL_OK)
-        st = sl::resolve_workers(desc, true, &nw_fp8, true);
-    if (st != SL_OK)
-        return st;
-    if (nw_fp8 > nw)
-        nw = nw_fp8;
+    // As sl_decode_attn_workspace_size's.
+    int nw = 0;
+    for (int kv = sl::kBf16; kv <= sl::kFp4; ++kv) {
+        int n = 0;
+        st = sl::resolve_workers(desc, kv, &n, true);
+        if (st != SL_OK)
+            return st;
+        nw = n > nw ? n : nw;
+    }
     *bytes = sl::prefix_workspace_layout(nullptr, desc->batch, desc->max_blocks_per_seq, desc->num_kv_heads,
                                          desc->num_q_heads / desc->num_kv_heads, desc->head_dim, nw, num_groups,
                                          nullptr);

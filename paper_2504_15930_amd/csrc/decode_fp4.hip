@@ -7,18 +7,18 @@
 namespace sl {
 namespace {
 
-template <int D>
+template <int D, int KV>
 __global__ __launch_bounds__(kWave * kWavesPerBlock) void split_fp4_kernel(SplitParams p)
 {
     extern __shared__ int32_t s_dyn[];
     int32_t *const s_cum = s_dyn;                // [B + 1]
     int32_t *const s_len = s_dyn + p.batch + 1;  // [B]
-    scan_sequences<step_tiles<D, kFp4>()>(p, s_cum, s_len);
+    scan_sequences<step_tiles<D, KV>()>(p, s_cum, s_len);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    split_unit_worker<D, kFp4, kAllPages>(p, wave * (int)gridDim.x + (int)blockIdx.x, StreamLds{s_cum, s_len});
+    split_unit_worker<D, KV, kAllPages>(p, wave * (int)gridDim.x + (int)blockIdx.x, StreamLds{s_cum, s_len});
 }
 
-template <int D>
+template <int D, int KV>
 __global__ __launch_bounds__(kWave * kWavesPerBlock) void prefix_fp4_kernel(SplitParams own, SplitParams shared,
                                                                                PrefixParams pp, int own_blocks,
                                                                                int max_shared)
@@ -34,10 +34,10 @@ __global__ __launch_bounds__(kWave * kWavesPerBlock) void prefix_fp4_kernel(Spli
     static_assert(sizeof(int32_t) * (2 * kMaxPrefixBatch + 1) <= kWavesPerBlock * kOwnStageBytes, "the group arrays");
     int32_t *const s_gs = reinterpret_cast<int32_t *>(own_state_stage());   // [NG + 1]
     int32_t *const s_sp = s_gs + pp.num_groups + 1;                         // [NG]
-    constexpr int NT = step_tiles<D, kFp4>();
+    constexpr int NT = step_tiles<D, KV, true>();
     scan_prefix_groups<NT>(own, pp, s_own, s_len, s_shared, s_sh, s_gl, s_gs, s_sp);
     if ((int)blockIdx.x < own_blocks)
-        split_unit_worker<D, kFp4, kOwnPages>(
+        split_unit_worker<D, KV, kOwnPages>(
             own, blockIdx.x * kWavesPerBlock + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave),
             StreamLds{s_own, s_len, s_shared});
     else {
@@ -52,14 +52,22 @@ __global__ __launch_bounds__(kWave * kWavesPerBlock) void prefix_fp4_kernel(Spli
 
 }  // namespace
 
-SplitKernel split_fp4_kernel_of(int head_dim)
+SplitKernel split_fp4_kernel_of(int head_dim, int group)
 {
-    return head_dim == 128 ? split_fp4_kernel<128> : head_dim == 64 ? split_fp4_kernel<64> : nullptr;
+    if (head_dim == 128)
+        return group <= 8 ? split_fp4_kernel<128, kFp4Half> : split_fp4_kernel<128, kFp4>;
+    if (head_dim == 64)
+        return group <= 8 ? split_fp4_kernel<64, kFp4Half> : split_fp4_kernel<64, kFp4>;
+    return nullptr;
 }
 
-PrefixKernel prefix_fp4_kernel_of(int head_dim)
+PrefixKernel prefix_fp4_kernel_of(int head_dim, int group)
 {
-    return head_dim == 128 ? prefix_fp4_kernel<128> : head_dim == 64 ? prefix_fp4_kernel<64> : nullptr;
+    if (head_dim == 128)
+        return group <= 8 ? prefix_fp4_kernel<128, kFp4Half> : prefix_fp4_kernel<128, kFp4>;
+    if (head_dim == 64)
+        return group <= 8 ? prefix_fp4_kernel<64, kFp4Half> : prefix_fp4_kernel<64, kFp4>;
+    return nullptr;
 }
 
 }  // namespace sl

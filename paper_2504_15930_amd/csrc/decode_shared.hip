@@ -86,7 +86,7 @@ hipError_t launch_prefix_split(const SplitParams &own, const SplitParams &shared
     const size_t lds = prefix_dynamic_lds(own.batch, pp.max_sub);
     PrefixKernel kernel = nullptr;
     if (kv == kFp4)
-        kernel = prefix_fp4_kernel_of(head_dim);
+        kernel = prefix_fp4_kernel_of(head_dim, own.group);
     else if (head_dim == 128)
         kernel = kv == kE4m3 ? prefix_split_kernel<128, true> : prefix_split_kernel<128, false>;
     else if (head_dim == 64)

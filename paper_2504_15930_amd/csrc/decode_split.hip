@@ -27,10 +27,10 @@ __global__ __launch_bounds__(kWave * kWavesPerBlock) void split_kv_kernel(SplitP
                                          StreamLds{s_cum, s_len});
 }
 
-SplitKernel split_kernel(int head_dim, int kv)
+SplitKernel split_kernel(int head_dim, int kv, int group)
 {
     if (kv == kFp4)
-        return split_fp4_kernel_of(head_dim);
+        return split_fp4_kernel_of(head_dim, group);
     if (head_dim == 128)
         return kv == kE4m3 ? split_kv_kernel<128, true> : split_kv_kernel<128, false>;
     if (head_dim == 64)
@@ -44,7 +44,7 @@ hipError_t launch_split(const SplitParams &p, int head_dim, int kv, hipStream_t 
 {
     const dim3 grid((p.num_workers + kWavesPerBlock - 1) / kWavesPerBlock);
     const dim3 block(kWave * kWavesPerBlock);
-    const SplitKernel kernel = split_kernel(head_dim, kv);
+    const SplitKernel kernel = split_kernel(head_dim, kv, p.group);
     if (!kernel)
         return hipErrorInvalidValue;
     hipLaunchKernelGGL(kernel, grid, block, split_dynamic_lds(p.batch), stream, p);
@@ -53,18 +53,20 @@ hipError_t launch_split(const SplitParams &p, int head_dim, int kv, hipStream_t 
 
 hipError_t split_blocks_per_cu(int head_dim, int kv, int *blocks)
 {
-    const SplitKernel kernel = split_kernel(head_dim, kv);
+    const SplitKernel kernel = split_kernel(head_dim, kv, kMaxGroup);
     if (!kernel)
         return hipErrorInvalidValue;
     return hipOccupancyMaxActiveBlocksPerMultiprocessor(blocks, kernel, kWave * kWavesPerBlock, 0);
 }
 
-int split_step_tiles(int head_dim, int kv)
+int split_step_tiles(int head_dim, int kv, bool prefix)
 {
     const bool d64 = head_dim == 64;
-    return kv == kFp4    ? d64 ? step_tiles<64, kFp4>() : step_tiles<128, kFp4>()
-           : kv == kE4m3 ? d64 ? step_tiles<64, kE4m3>() : step_tiles<128, kE4m3>()
-                         : d64 ? step_tiles<64, kBf16>() : step_tiles<128, kBf16>();
+    if (kv == kFp4)
+        return prefix ? (d64 ? step_tiles<64, kFp4, true>() : step_tiles<128, kFp4, true>())
+                      : (d64 ? step_tiles<64, kFp4>() : step_tiles<128, kFp4>());
+    return kv == kE4m3 ? (d64 ? step_tiles<64, kE4m3>() : step_tiles<128, kE4m3>())
+                       : (d64 ? step_tiles<64, kBf16>() : step_tiles<128, kBf16>());
 }
 
 }  // namespace sl

@@ -50,27 +50,14 @@
 // LDS. The codes are widened to bf16 with their block's power of two
 // (v_cvt_scalef32_pk_bf16_fp4, exact), so scores and weights are as for a bf16
 // cache.
-#include "fp4_unit.h"
-#include "sl_internal.h"
-#include "wave_ops.h"
+#include <type_traits>
+
+#include "fp4_step.h"
+#include "unit_ops.h"
 
 namespace sl {
 namespace {
 
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-typedef short i16x4_t __attribute__((ext_vector_type(4)));
-typedef float f32x4_t __attribute__((ext_vector_type(4)));
-typedef float f32x2_t __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
-
-constexpr float kNegInf = -__builtin_inff();
-// A partial state l = sum 2^(s - m), acc = sum 2^(s - m) v is exact for any
-// reference m. The running maximum is raised only when a score exceeds it by
-// more than this slack (base-2 units), which bounds the weights by 2^8 and
-// leaves the accumulators untouched on most tiles after a unit's first.
-constexpr float kRescaleSlack = 8.0f;
 // Tiles per pipeline step and steps in flight. A worker is one wavefront, most
 // often alone on its SIMD, so its chain of dependent instructions per tile is
 // time that nothing fills: at 1024 workers a wavefront has ~0.65 us for an
@@ -82,43 +69,23 @@ constexpr float kRescaleSlack = 8.0f;
 //   bf16 D = 64, 384 x 1..2048 tokens, 8 KV heads   165 -> 130 us (with 1024 workers)
 //   E4M3 D = 128, 512 x 512 + lognormal(2048)        319 -> 316 us; at 768 workers 381 -> 327
 //   E4M3 D = 64, 384 x 1..4096 tokens, 8 KV heads   226 -> 146 us (two tiles: 157)
+// FP4: four tiles per step carry as much as two of E4M3 (two per step: 512 x 512 +
+// lognormal(2048), 28/4 heads, 191 us instead of 172), but not in the prefix
+// kernel, where the registers of four leave no room for a shared-page workgroup
+// beside an own-page one (32 prompts x 8 samples, 59 us instead of 43).
 // Two steps in flight; three were no faster anywhere (and slower where they
 // cost a resident workgroup, in the prefix kernel).
-template <int D, int KV>
-constexpr int step_tiles() { return KV == kFp4 ? 4 : D == 64 ? (KV == kE4m3 ? 4 : 2) : (KV == kE4m3 ? 2 : 1); }
-constexpr int kPipelineDepth = 2;
-constexpr int kRawBufferWord3 = 0x00020000;  // untyped 32-bit buffer resource (CDNA3/4)
-
-// Two fp32 -> packed bf16 pair, round to nearest even (v_cvt_pk_bf16_f32).
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+template <int D, int KV, bool PREFIX = false>
+constexpr int step_tiles()
 {
-    f32x2_t v = {lo, hi};
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
+    return is_fp4(KV) ? (PREFIX ? 2 : 4) : D == 64 ? (KV == kE4m3 ? 4 : 2) : (KV == kE4m3 ? 2 : 1);
 }
-
-__device__ __forceinline__ float bf16_lo(uint32_t w) { return __builtin_bit_cast(float, w << 16); }
-__device__ __forceinline__ float bf16_hi(uint32_t w) { return __builtin_bit_cast(float, w & 0xffff0000u); }
-
+constexpr int kPipelineDepth = 2;
 // Four E4M3 codes (one dword) -> four bf16 (two dwords), exact.
 __device__ __forceinline__ void e4m3x4_to_bf16(uint32_t codes, uint32_t &lo, uint32_t &hi)
 {
     lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.0f, false));
     hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.0f, true));
-}
-
-// Max / sum over the lanes n, n + 16, n + 32, n + 48 of a column.
-// (The gfx950 lane-swap builtins would avoid the LDS crossbar here, but this
-// compiler folds max(h[0], h[1]) of their two results to one of them, so the
-// plain shuffles are used.)
-__device__ __forceinline__ float quad_max(float x)
-{
-    x = fmaxf(x, __shfl_xor(x, 16, kWave));
-    return fmaxf(x, __shfl_xor(x, 32, kWave));
-}
-__device__ __forceinline__ float quad_sum(float x)
-{
-    x += __shfl_xor(x, 16, kWave);
-    return x + __shfl_xor(x, 32, kWave);
 }
 
 template <int D, int KV>
@@ -131,13 +98,10 @@ struct Tile {
     float scl;           // FP8: key scale in lanes 0-31, value scale in lanes 32-63
 };
 template <int D>
-struct Tile<D, kFp4> {
-    static constexpr int KW = D / 32;
-    static constexpr int VW = D / 32;
-    uint32_t k[KW];
-    uint32_t v[VW];
-    uint32_t ks;         // the scale byte of the lane's key elements
-    uint32_t vs;         // those of its value elements in rows 4 quad + r, byte r
+struct Tile<D, kFp4> : Fp4Tile<D> {
+};
+template <int D>
+struct Tile<D, kFp4Half> : Fp4Tile<D> {
 };
 
 // One pipeline step: NT consecutive tiles of one unit (fewer at the unit's end).
@@ -154,16 +118,6 @@ template <int D, int KV>
 __device__ __forceinline__ int q_index(int s, int quad)
 {
     return KV == kBf16 ? 32 * s + 8 * quad : quad * (D / 4) + 8 * s;
-}
-
-// K/V pages are read exactly once per call: stream them with non-temporal loads
-// so they do not displace reusable lines in L2 / the Infinity Cache (measured on
-// MI355X: random 4 KB tiles reach ~6.8 TB/s this way, ~6.0 TB/s with plain loads).
-constexpr int kCachePolicyStream = 2;   // NT
-
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *base, uint32_t bytes)
-{
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, (int)bytes, kRawBufferWord3);
 }
 
 // The score-MFMA B operands of a unit with first query row row0, zero where
@@ -240,61 +194,13 @@ __device__ __forceinline__ void issue_tile(Tile<D, KV> &t, const SplitParams &p,
     }
 }
 
-// The same of an FP4 record: codes as operands lie in it, and the lane's scales.
-template <int D, bool STREAM>
-__device__ __forceinline__ void issue_record(Tile<D, kFp4> &t, const SplitParams &p, uint32_t tile, bool read, int n,
-                                             int quad, int lane)
+// The query rows of a step's unit: `blk` < 0: a single-unit step, whose query
+// rows are the group's G heads; `blk` >= 0: column block blk of a shared unit
+// (rows 16 blk + n, member r / G and head r % G of the group).
+template <int D, int KV, int NT>
+__device__ __forceinline__ void issue_query(Step<D, KV, NT> &st, const SplitParams &p, bool with_q, int n, int quad,
+                                            int blk)
 {
-    constexpr int kPolicy = STREAM ? kCachePolicyStream : 0;
-    using L = Fp4Layout<D>;
-    const __amdgpu_buffer_rsrc_t rec = buffer_of(static_cast<const uint8_t *>(p.k_pages) + (size_t)tile * L::kBytes,
-                                                 read ? (uint32_t)L::kBytes : 0u);
-    if constexpr (D == 128) {
-        const u32x4_t k =
-            __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rec, 16 * lane, 0, kPolicy));
-        const u32x4_t v =
-            __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rec, L::kV + 16 * lane, 0, kPolicy));
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            t.k[c] = k[c];
-            t.v[c] = v[c];
-        }
-    } else {   // half a block of 32 key elements per lane
-        const u32x2_t k = __builtin_bit_cast(
-            u32x2_t,
-            __builtin_amdgcn_raw_buffer_load_b64(rec, L::k_code(n, quad >> 1) + 8 * (quad & 1), 0, kPolicy));
-        const u32x2_t v =
-            __builtin_bit_cast(u32x2_t, __builtin_amdgcn_raw_buffer_load_b64(rec, L::kV + 8 * lane, 0, kPolicy));
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            t.k[c] = k[c];
-            t.v[c] = v[c];
-        }
-    }
-    t.ks = __builtin_amdgcn_raw_buffer_load_b8(rec, L::k_scale(n, D == 128 ? quad : quad >> 1), 0, kPolicy);
-    t.vs = __builtin_bit_cast(
-        uint32_t, __builtin_amdgcn_raw_buffer_load_b32(rec, L::v_scale(4 * quad, n * (D / 16) / 32), 0, kPolicy));
-}
-
-// Issue the loads of a step: tiles T[u] (a page-head tile index, or the
-// complement ~i of one for a tile that is not to be read: past the unit's end
-// or in a page outside the pool; its scales are those of tile i) and, `with_q`,
-// the unit's query rows. `live` false: a step past the range, nothing is read.
-// `blk` < 0: a single-unit step, whose query rows are the group's G heads;
-// `blk` >= 0: column block blk of a shared unit (rows 16 blk + n, member r / G
-// and head r % G of the group).
-template <int D, int KV, int NT, bool STREAM>
-__device__ __forceinline__ void issue_step(Step<D, KV, NT> &st, const SplitParams &p, const int32_t (&T)[NT],
-                                           bool live, bool with_q, int n, int quad, int lane, int blk)
-{
-#pragma unroll
-    for (int u = 0; u < NT; ++u) {
-        const uint32_t at = (uint32_t)(T[u] ^ (T[u] >> 31));
-        if constexpr (KV == kFp4)
-            issue_record<D, STREAM>(st.t[u], p, at, live && T[u] >= 0, n, quad, lane);
-        else
-            issue_tile<D, KV, STREAM>(st.t[u], p, at, live && T[u] >= 0, n, quad, lane);
-    }
     const uint32_t row0 = (st.meta >> kMetaUnitShift) * (uint32_t)p.group;
     if (blk < 0) {
         // One tile per step: the q loads are issued only where they read
@@ -304,7 +210,7 @@ __device__ __forceinline__ void issue_step(Step<D, KV, NT> &st, const SplitParam
         // step once per unit, which costs the others more (D = 64 bf16, 130
         // against 137 us; E4M3 D = 128, 313 against 316).
         if (NT > 1 || with_q)
-            load_q<D, KV>(st.q, p, row0, with_q, n, quad);
+            load_q<D, KV>(st.q, p, row0, with_q, KV == kFp4Half ? n & 7 : n, quad);
     } else if (with_q) {
         // Issued for a unit's first step only: four wavefronts load every tile
         // here, from L2, and with two such workgroups on a CU the load
@@ -322,6 +228,20 @@ __device__ __forceinline__ void issue_step(Step<D, KV, NT> &st, const SplitParam
                 u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(
                              qr, (int)(2u * (rel * (uint32_t)D + (uint32_t)q_index<D, KV>(s, quad))), 0, 0));
     }
+}
+
+// Issue the loads of a step: tiles T[u] (a page-head tile index, or the
+// complement ~i of one for a tile that is not to be read: past the unit's end
+// or in a page outside the pool; its scales are those of tile i) and, `with_q`,
+// the unit's query rows. `live` false: a step past the range, nothing is read.
+template <int D, int KV, int NT, bool STREAM>
+__device__ __forceinline__ void issue_step(Step<D, KV, NT> &st, const SplitParams &p, const int32_t (&T)[NT],
+                                           bool live, bool with_q, int n, int quad, int lane, int blk)
+{
+#pragma unroll
+    for (int u = 0; u < NT; ++u)
+        issue_tile<D, KV, STREAM>(st.t[u], p, (uint32_t)(T[u] ^ (T[u] >> 31)), live && T[u] >= 0, n, quad, lane);
+    issue_query<D, KV, NT>(st, p, with_q, n, quad, blk);
 }
 
 // Regroup the K tiles (loaded as whole 1 KB runs) into the score-MFMA layout
@@ -382,31 +302,6 @@ __device__ __forceinline__ bf16x8_t k_operand(const u32x4_t (&kc)[KV == kE4m3 ? 
     return __builtin_bit_cast(bf16x8_t, w);
 }
 
-// The same for an FP4 record: dword s of the lane's codes, with their block's scale.
-template <int D>
-__device__ __forceinline__ bf16x8_t k_operand_fp4(const Tile<D, kFp4> &t, float scale, int s)
-{
-    return __builtin_bit_cast(bf16x8_t, u32x4_t{fp4x2_to_bf16<0>(t.k[s], scale), fp4x2_to_bf16<1>(t.k[s], scale),
-                                                fp4x2_to_bf16<2>(t.k[s], scale), fp4x2_to_bf16<3>(t.k[s], scale)});
-}
-
-template <int D>
-struct Piece {
-    f32x4_t acc[D / 16];
-    float m;   // running max of this lane's head, base-2 units
-    float l;   // this lane's share of the sum of (bf16-rounded) weights
-};
-
-template <int D>
-__device__ __forceinline__ void reset(Piece<D> &st)
-{
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i)
-        st.acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    st.m = kNegInf;
-    st.l = 0.f;
-}
-
 // One step of the online softmax over the first NT of its tiles. `valid` = live
 // tokens of the step (1 .. 16 NT; the first tile has at least one).
 //
@@ -422,26 +317,17 @@ __device__ __forceinline__ void compute_step(Piece<D> &st, const Tile<D, KV> (&t
                                              int lane, int n, int quad)
 {
     static_assert(NT == 1 || NT % 2 == 0, "one tile, or pairs of tiles, per step");
+    u32x4_t kc[NT][KV == kE4m3 ? D / 64 : D / 32];
+    regroup_k<D, KV, NT>(t, lds, lane, n, quad, kc);
     f32x4_t s4[NT];
 #pragma unroll
     for (int u = 0; u < NT; ++u)
         s4[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    if constexpr (KV == kFp4) {
 #pragma unroll
-        for (int s = 0; s < D / 32; ++s)
+    for (int s = 0; s < D / 32; ++s)
 #pragma unroll
-            for (int u = 0; u < NT; ++u)
-                s4[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k_operand_fp4<D>(t[u], e8m0(t[u].ks), s), qop[s], s4[u],
-                                                                0, 0, 0);
-    } else {
-        u32x4_t kc[NT][KV == kE4m3 ? D / 64 : D / 32];
-        regroup_k<D, KV, NT>(t, lds, lane, n, quad, kc);
-#pragma unroll
-        for (int s = 0; s < D / 32; ++s)
-#pragma unroll
-            for (int u = 0; u < NT; ++u)
-                s4[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k_operand<D, KV>(kc[u], s), qop[s], s4[u], 0, 0, 0);
-    }
+        for (int u = 0; u < NT; ++u)
+            s4[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k_operand<D, KV>(kc[u], s), qop[s], s4[u], 0, 0, 0);
 
     float vmul[NT];
     float sc[NT][4];
@@ -533,53 +419,28 @@ __device__ __forceinline__ void compute_step(Piece<D> &st, const Tile<D, KV> (&t
     // rows before one widening per two blocks. Dead slots (only in a
     // sequence's last page) hold arbitrary cache contents and are zeroed first,
     // as 0 * NaN would poison the MFMA.
-    // FP4 codes are finite whatever they are, and a dead slot's are only kept from
-    // an infinite or NaN scale: it takes the scale 1.
-    constexpr int VR = KV == kFp4 ? 1 : Tile<D, KV>::VW / 4;   // dwords per row
+    constexpr int VR = Tile<D, KV>::VW / 4;   // dwords per row
     uint32_t vr[NT][4 * VR];
-    float vscale[NT][4];   // FP4: of the lane's block in each row
-    if constexpr (KV == kFp4) {
+#pragma unroll
+    for (int u = 0; u < NT; ++u)
+#pragma unroll
+        for (int k = 0; k < 4 * VR; ++k)
+            vr[u][k] = t[u].v[k];
+    if (valid < kPageSize * NT) {
 #pragma unroll
         for (int u = 0; u < NT; ++u)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                vscale[u][r] = e8m0(t[u].vs >> (8 * r));
-                if (valid < kPageSize * NT && kPageSize * u + 4 * quad + r >= valid)
-                    vscale[u][r] = 1.0f;
-                vr[u][r] = D == 128 ? t[u].v[r] : t[u].v[r / 2] >> (16 * (r % 2));
-            }
-    } else {
+            for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int u = 0; u < NT; ++u)
-#pragma unroll
-            for (int k = 0; k < 4 * VR; ++k)
-                vr[u][k] = t[u].v[k];
-        if (valid < kPageSize * NT) {
-#pragma unroll
-            for (int u = 0; u < NT; ++u)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-#pragma unroll
-                    for (int c = 0; c < VR; ++c)
-                        vr[u][r * VR + c] = kPageSize * u + 4 * quad + r < valid ? vr[u][r * VR + c] : 0u;
-        }
+                for (int c = 0; c < VR; ++c)
+                    vr[u][r * VR + c] = kPageSize * u + 4 * quad + r < valid ? vr[u][r * VR + c] : 0u;
     }
 #pragma unroll
     for (int i = 0; i < D / 16; i += 2) {
         uint32_t a0[2 * NT], a1[2 * NT];   // operands of blocks i and i + 1
 #pragma unroll
         for (int u = 0; u < NT; ++u) {
-            if constexpr (KV == kFp4) {
-                // A byte holds elements i and i + 1 of a row.
-                uint32_t w[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    w[r] = fp4x2_to_bf16_at(vr[u][r], vscale[u][r], i / 2);
-                a0[2 * u] = __builtin_amdgcn_perm(w[1], w[0], 0x05040100u);
-                a1[2 * u] = __builtin_amdgcn_perm(w[1], w[0], 0x07060302u);
-                a0[2 * u + 1] = __builtin_amdgcn_perm(w[3], w[2], 0x05040100u);
-                a1[2 * u + 1] = __builtin_amdgcn_perm(w[3], w[2], 0x07060302u);
-            } else if constexpr (KV == kE4m3) {
+            if constexpr (KV == kE4m3) {
                 // Bytes (row a, row b) of elements i and i + 1, then one widening per element.
                 const int c = i / 4;
                 const uint32_t sel = (i % 4) == 0 ? 0x05010400u : 0x07030602u;
@@ -934,7 +795,7 @@ __device__ __forceinline__ void scan_sequences(const SplitParams &p, int32_t *s_
 template <int D, int KV>
 __device__ __forceinline__ uint8_t *k_regroup_stage()
 {
-    if constexpr (KV == kFp4)
+    if constexpr (is_fp4(KV))
         return nullptr;   // nothing is regrouped
     __shared__ __attribute__((aligned(16)))
     uint8_t k_stage[kWavesPerBlock][kPageSize * D * (KV == kE4m3 ? 1 : 2)];
@@ -972,7 +833,7 @@ __device__ __forceinline__ void split_unit_worker(const SplitParams &p, int w, c
     if (w >= p.num_workers)
         return;
     const int nseq = kShared ? sv.num_groups : p.batch;   // "sequences" of the stream
-    constexpr int NT = step_tiles<D, KV>();
+    constexpr int NT = step_tiles<D, KV, MODE != kAllPages>();
     const int Hkv = p.num_kv_heads;
     const long long total = (long long)sv.cum[nseq] * Hkv;
     const int nw = effective_workers(total, p.num_workers, NT, kShared ? 0 : wide_from(p.num_workers, KV));
@@ -1066,6 +927,7 @@ __device__ __forceinline__ void split_unit_worker(const SplitParams &p, int w, c
         return d;
     };
     int32_t tile[NT];     // per lane: issue_step's T of the lane's step
+    uint64_t rec[NT];     // FP4 instead: the addresses of its records (those that are not to be read: its first one's)
     uint32_t lmeta;       // its metadata (kMetaBad also for a page outside the pool)
     int32_t lvalid;
     auto settle = [&](const Desc &d) {
@@ -1074,7 +936,12 @@ __device__ __forceinline__ void split_unit_worker(const SplitParams &p, int w, c
         for (int u = 0; u < NT; ++u) {
             const bool in = (uint32_t)d.bt[u] < (uint32_t)p.num_pages, has = u < d.tiles;
             const int32_t at = d.bt[u] * Hkv + d.g;
-            tile[u] = has && in ? at : ~(u > 0 ? tile[0] ^ (tile[0] >> 31) : 0);
+            if constexpr (is_fp4(KV)) {
+                const uint64_t base = reinterpret_cast<uint64_t>(p.k_pages);
+                rec[u] = has && in ? base + (uint64_t)(uint32_t)at * (uint32_t)fp4_record_bytes(D) : u > 0 ? rec[0] : base;
+            } else {
+                tile[u] = has && in ? at : ~(u > 0 ? tile[0] ^ (tile[0] >> 31) : 0);
+            }
             bad |= has && !in;
         }
         lmeta = d.meta | (bad ? kMetaBad : 0u);
@@ -1085,12 +952,26 @@ __device__ __forceinline__ void split_unit_worker(const SplitParams &p, int w, c
     settle(ahead);
     auto issue = [&](Step<D, KV, NT> &x, int i, bool with_q) {   // step i of the range, from lane cpos
         int32_t T[NT];
+        uint64_t R[NT];
 #pragma unroll
-        for (int u = 0; u < NT; ++u)
-            T[u] = __builtin_amdgcn_readlane(tile[u], cpos);
+        for (int u = 0; u < NT; ++u) {
+            if constexpr (is_fp4(KV))
+                R[u] = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)rec[u], cpos) |
+                       (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(rec[u] >> 32), cpos) << 32;
+            else
+                T[u] = __builtin_amdgcn_readlane(tile[u], cpos);
+        }
         x.meta = (uint32_t)__builtin_amdgcn_readlane((int)lmeta, cpos);
         x.valid = __builtin_amdgcn_readlane(lvalid, cpos);
-        issue_step<D, KV, NT, !kShared>(x, p, T, i < nsteps, with_q || (x.meta & kMetaFirst) != 0, n, quad, lane, blk);
+        with_q = with_q || (x.meta & kMetaFirst) != 0;
+        if constexpr (is_fp4(KV)) {
+#pragma unroll
+            for (int u = 0; u < NT; ++u)
+                issue_record<D, kShared ? 0 : kCachePolicyStream>(x.t[u], R[u], i < nsteps, n, quad, lane);
+            issue_query<D, KV, NT>(x, p, with_q, n, quad, blk);
+        } else {
+            issue_step<D, KV, NT, !kShared>(x, p, T, i < nsteps, with_q, n, quad, lane, blk);
+        }
         ++cpos;
     };
 
@@ -1102,8 +983,8 @@ __device__ __forceinline__ void split_unit_worker(const SplitParams &p, int w, c
     if (nsteps > kChunk)
         ahead = find(kChunk);
 
-    Piece<D> st;
-    reset(st);
+    std::conditional_t<is_fp4(KV), Fp4State<D, KV == kFp4Half>, Piece<D>> state;
+    reset(state);
     bf16x8_t qop[D / 32];   // score-MFMA B operands of the current unit (zero columns past its rows)
     bool started = false;   // the current unit's first tile is inside this range
     bool bad = false;
@@ -1127,7 +1008,7 @@ __device__ __forceinline__ void split_unit_worker(const SplitParams &p, int w, c
                 if (i == 0 || (meta & kMetaFirst) != 0) {
 #pragma unroll
                     for (int s = 0; s < D / 32; ++s)
-                        qop[s] = __builtin_bit_cast(bf16x8_t, t.q[s]);
+                        qop[s] = __builtin_bit_cast(bf16x8_t, is_fp4(KV) ? t.q[s] ^ fp4_sign(p.scale_log2) : t.q[s]);
                 }
                 started |= (meta & kMetaFirst) != 0;
                 bad |= (meta & kMetaBad) != 0;
@@ -1140,15 +1021,26 @@ __device__ __forceinline__ void split_unit_worker(const SplitParams &p, int w, c
                 // are long: their loop lost 5%.)
                 constexpr bool kFew = NT == 4 && !kShared;
                 const int valid = kShared ? t.valid & 0xff : t.valid;
-                if (kFew && (meta & kMetaLast) == 0)
-                    compute_step<D, KV, NT>(st, t.t, qop, p.scale_log2, kPageSize * NT, lds, lane, n, quad);
+                if constexpr (is_fp4(KV)) {
+                    const float mul = __builtin_fabsf(p.scale_log2);
+                    if (kFew && (meta & kMetaLast) == 0)
+                        fp4_step<D, NT>(state, t.t, qop, mul, kPageSize * NT, n, quad);
+                    else if (kFew && valid <= kPageSize)
+                        fp4_step<D, 1>(state, t.t, qop, mul, valid, n, quad);
+                    else if (kFew && valid <= 2 * kPageSize)
+                        fp4_step<D, 2>(state, t.t, qop, mul, valid, n, quad);
+                    else
+                        fp4_step<D, NT>(state, t.t, qop, mul, valid, n, quad);
+                } else if (kFew && (meta & kMetaLast) == 0)
+                    compute_step<D, KV, NT>(state, t.t, qop, p.scale_log2, kPageSize * NT, lds, lane, n, quad);
                 else if (kFew && valid <= kPageSize)
-                    compute_step<D, KV, 1>(st, t.t, qop, p.scale_log2, valid, lds, lane, n, quad);
+                    compute_step<D, KV, 1>(state, t.t, qop, p.scale_log2, valid, lds, lane, n, quad);
                 else if (kFew && valid <= 2 * kPageSize)
-                    compute_step<D, KV, 2>(st, t.t, qop, p.scale_log2, valid, lds, lane, n, quad);
+                    compute_step<D, KV, 2>(state, t.t, qop, p.scale_log2, valid, lds, lane, n, quad);
                 else
-                    compute_step<D, KV, NT>(st, t.t, qop, p.scale_log2, valid, lds, lane, n, quad);
+                    compute_step<D, KV, NT>(state, t.t, qop, p.scale_log2, valid, lds, lane, n, quad);
                 if (kShared && ((meta & kMetaLast) != 0 || ends)) {
+                    auto &&st = finished(state, quad);
                     // A shared unit's state is always merged: a whole one goes to the unit area
                     // (indexed by first query row / G), a cut one to the worker's slot; block blk
                     // holds rows 16 blk .. 16 blk + 15 of the unit's kPrefixRows.
@@ -1160,11 +1052,12 @@ __device__ __forceinline__ void split_unit_worker(const SplitParams &p, int w, c
                     if (r < ((t.valid >> 8) + 1) * G)
                         store_partial<D>(st, l, bad, whole ? p.unit_ml : p.part_ml, whole ? p.unit_acc : p.part_acc,
                                          slot * kPrefixRows + r, quad);
-                    reset(st);
+                    reset(state);
                     started = false;
                     bad = false;
                     slot_sel = 1;
                 } else if (!kShared && ((meta & kMetaLast) != 0 || ends)) {
+                    auto &&st = finished(state, quad);
                     // A unit cut by this range leaves its piece in the worker's slot 2w + slot_sel.
                     // A whole unit is written out, unless it still has to be merged (shared pages,
                     // or the own pages of a sequence that has them): then its state goes to its
@@ -1206,7 +1099,7 @@ __device__ __forceinline__ void split_unit_worker(const SplitParams &p, int w, c
                     } else {
                         finish_unit<D>(p, st, row0, whole && !to_unit, bad, pml, pacc, slot, n, quad);
                     }
-                    reset(st);
+                    reset(state);
                     started = false;
                     bad = false;
                     slot_sel = 1;

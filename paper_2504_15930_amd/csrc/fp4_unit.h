@@ -47,6 +47,18 @@ struct Fp4Layout {
 // field it is (the conversion below reads 255 as NaN and 0 as 2^-127).
 __device__ __forceinline__ float e8m0(uint32_t x) { return __builtin_bit_cast(float, (x & 0xffu) << 23); }
 
+// The same of byte B of x, in one instruction. (Left to itself the compiler takes
+// a shift and a mask.)
+template <int B>
+__device__ __forceinline__ float e8m0_byte(uint32_t x)
+{
+    float f;
+    asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_%3"
+        : "=v"(f)
+        : "v"(23), "v"(x), "i"(B));
+    return f;
+}
+
 // The two codes of byte B of x, times `scale`, as a bf16 pair (low half: the
 // low code), exact.
 template <int B>

@@ -46,6 +46,9 @@ constexpr int kPageSize = 16;
 // What a cache's pages hold: bf16 rows, E4M3 codes with a scale per page-head
 // tile, or the records of fp4_unit.h (E2M1 codes with a scale per 32 elements).
 enum Kv : int { kBf16 = 0, kE4m3 = 1, kFp4 = 2 };
+// In the kernels alone: an FP4 cache and at most eight query heads per KV head (fp4_step.h).
+constexpr int kFp4Half = 3;
+__host__ __device__ constexpr bool is_fp4(int kv) { return kv >= kFp4; }
 constexpr size_t fp4_record_bytes(int head_dim) { return 17 * (size_t)head_dim; }
 constexpr int kWave = 64;
 constexpr int kWavesPerBlock = 4;          // split kernel: 4 independent workers per block
@@ -290,8 +293,8 @@ inline size_t prefix_dynamic_lds(int batch, int max_sub)
 }
 using SplitKernel = void (*)(SplitParams);
 using PrefixKernel = void (*)(SplitParams, SplitParams, PrefixParams, int, int);
-SplitKernel split_fp4_kernel_of(int head_dim);     // decode_fp4.hip (null: no such head_dim)
-PrefixKernel prefix_fp4_kernel_of(int head_dim);
+SplitKernel split_fp4_kernel_of(int head_dim, int group);     // decode_fp4.hip (null: no such head_dim)
+PrefixKernel prefix_fp4_kernel_of(int head_dim, int group);
 hipError_t launch_split(const SplitParams &p, int head_dim, int kv, hipStream_t stream);
 // Prefix mode: the own-page pass (single-unit workers) and the shared-page
 // pass (one workgroup of kPrefixBlocks wavefronts per worker, one 16-row
@@ -313,6 +316,7 @@ struct Fp4RowParams {
     const int32_t *slots, *block_table, *seq_lens;
     uint8_t *pages;   // [num_pages][Hkv][17 D]
     int32_t rows, num_kv_heads, max_blocks, num_pages;
+    uint32_t heads_inverse;   // inverse_of(num_kv_heads), or 0 (set by the launch)
 };
 hipError_t launch_fp4_rows(const Fp4RowParams &p, int head_dim, hipStream_t stream);
 // Page bookkeeping (pages.hip).
@@ -329,7 +333,7 @@ hipError_t launch_release_pages(const PageParams &p, hipStream_t stream);
 hipError_t launch_engine_fill(const int32_t *pages, int n_pages, int hkv, int head_dim, bool fp8, uint32_t seed,
                               void *k_pages, void *v_pages, float *k_scales, float *v_scales, hipStream_t stream);
 // Pages per pipeline step of the split kernels (their streams are counted in steps).
-int split_step_tiles(int head_dim, int kv);
+int split_step_tiles(int head_dim, int kv, bool prefix);
 // Resident split-kernel workgroups per CU (occupancy query), for the default worker count.
 hipError_t split_blocks_per_cu(int head_dim, int kv, int *blocks);
 
