@@ -25,23 +25,27 @@ typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 
 constexpr int kRowThreads = 256;
-constexpr int kPer = 8;   // elements per thread
+constexpr int kPer = 8;   // elements of a row per thread
+// From this many elements of K and V on (4096 workgroups with one row per thread),
+// rows per thread: fewer workgroups to start.
+constexpr long long kManyRowElements = 4ll << 20;
+constexpr int kRowsPerThread = 4;
 
-// Which element run of which row a thread has: `part` 0 .. D/8 - 1 of the key
-// (which 0) or value row of (token, KV head) number `unit`.
-template <int D>
+// Which element run of which rows a thread has: `part` 0 .. D/8 - 1 of the key
+// (which 0) or value row of the (token, KV head) numbers first, first + kUnits, ...
+template <int D, int ROWS>
 struct RowPart {
     static constexpr int kParts = D / kPer;
-    static constexpr int kUnits = kRowThreads / (2 * kParts);   // per workgroup
-    int unit;   // (the launch has fewer than 2^27)
-    int which, part;
+    static constexpr int kUnits = kRowThreads / (2 * kParts);
+    int first, which, part;
     __device__ __forceinline__ RowPart()
     {
         const int at = threadIdx.x;
         part = at % kParts;
         which = at / kParts % 2;
-        unit = (int)blockIdx.x * kUnits + at / (2 * kParts);
+        first = (int)blockIdx.x * (kUnits * ROWS) + at / (2 * kParts);
     }
+    __device__ __forceinline__ int unit(int i) const { return first + i * kUnits; }
 };
 
 // Maximum over the four threads of a block (neighbouring lanes).
@@ -134,61 +138,92 @@ __device__ __forceinline__ int slot_of(const Fp4RowParams &p, int t)
     return page < 0 || page >= p.num_pages ? -1 : page * kPageSize + (L - 1) % kPageSize;
 }
 
+// Token of a unit, unit / num_kv_heads (fewer than 2^27 units).
+__device__ __forceinline__ int token_of(const Fp4RowParams &p, int unit)
+{
+    return p.heads_inverse ? (int)__umulhi((uint32_t)unit, p.heads_inverse)
+                           : (int)((uint32_t)unit / (uint32_t)p.num_kv_heads);
+}
+
 template <int D>
 __device__ __forceinline__ size_t record_at(const Fp4RowParams &p, int slot, int g)
 {
     return ((size_t)(slot / kPageSize) * p.num_kv_heads + g) * Fp4Layout<D>::kBytes;
 }
 
-template <int D>
+// ROWS rows per thread, all of their loads under way before the first store.
+template <int D, int ROWS>
 __global__ __launch_bounds__(kRowThreads) void fp4_store_kernel(Fp4RowParams p)
 {
-    const RowPart<D> r;
-    const int t = r.unit / p.num_kv_heads;
-    if (t >= p.rows)
-        return;
-    const u32x4_t x = *reinterpret_cast<const u32x4_t *>((r.which ? p.v_rows : p.k_rows) + (size_t)r.unit * D + kPer * r.part);
-    const int slot = slot_of(p, t);
-    if (slot < 0 || slot >= p.num_pages * kPageSize)
-        return;
-    uint8_t *const rec = p.pages + record_at<D>(p, slot, r.unit - t * p.num_kv_heads);
-    store_part<D>(rec, r.which, slot % kPageSize, r.part, x);
+    const RowPart<D, ROWS> r;
+    const int units = p.rows * p.num_kv_heads;
+    u32x4_t x[ROWS];
+    int slot[ROWS], g[ROWS];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const int unit = min(r.unit(i), units - 1), t = token_of(p, unit);
+        g[i] = unit - t * p.num_kv_heads;
+        x[i] = *reinterpret_cast<const u32x4_t *>((r.which ? p.v_rows : p.k_rows) + (size_t)unit * D + kPer * r.part);
+        slot[i] = r.unit(i) < units ? slot_of(p, t) : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i)
+        if (slot[i] >= 0 && slot[i] < p.num_pages * kPageSize)
+            store_part<D>(p.pages + record_at<D>(p, slot[i], g[i]), r.which, slot[i] % kPageSize, r.part, x[i]);
 }
 
-template <int D>
+template <int D, int ROWS>
 __global__ __launch_bounds__(kRowThreads) void fp4_load_kernel(Fp4RowParams p)
 {
-    const RowPart<D> r;
-    const int t = r.unit / p.num_kv_heads;
-    if (t >= p.rows)
-        return;
-    const int slot = p.slots[t];
-    u32x4_t x = {0u, 0u, 0u, 0u};
-    if (slot >= p.num_pages * kPageSize)
-        x = u32x4_t{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
-    else if (slot >= 0)
-        x = load_part<D>(p.pages + record_at<D>(p, slot, r.unit - t * p.num_kv_heads), r.which,
-                         slot % kPageSize, r.part);
-    *reinterpret_cast<u32x4_t *>((r.which ? p.v_out : p.k_out) + (size_t)r.unit * D + kPer * r.part) = x;
+    const RowPart<D, ROWS> r;
+    const int units = p.rows * p.num_kv_heads;
+    int slot[ROWS], g[ROWS];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const int unit = min(r.unit(i), units - 1), t = token_of(p, unit);
+        g[i] = unit - t * p.num_kv_heads;
+        slot[i] = p.slots[t];
+    }
+    u32x4_t x[ROWS];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const bool in = slot[i] >= 0 && slot[i] < p.num_pages * kPageSize;
+        const uint32_t none = slot[i] < 0 ? 0u : 0x7fc07fc0u;
+        x[i] = u32x4_t{none, none, none, none};
+        if (in)
+            x[i] = load_part<D>(p.pages + record_at<D>(p, slot[i], g[i]), r.which, slot[i] % kPageSize, r.part);
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i)
+        if (r.unit(i) < units)
+            *reinterpret_cast<u32x4_t *>((r.which ? p.v_out : p.k_out) + (size_t)r.unit(i) * D + kPer * r.part) = x[i];
 }
 
-template <int D>
+template <int D, int ROWS>
 hipError_t launch(const Fp4RowParams &p, hipStream_t stream)
 {
-    const long long units = (long long)p.rows * p.num_kv_heads;
-    const dim3 grid((unsigned)((units + RowPart<D>::kUnits - 1) / RowPart<D>::kUnits)), block(kRowThreads);
+    const long long units = (long long)p.rows * p.num_kv_heads, per = RowPart<D, ROWS>::kUnits * ROWS;
+    const dim3 grid((unsigned)((units + per - 1) / per)), block(kRowThreads);
     if (p.k_rows)
-        hipLaunchKernelGGL(fp4_store_kernel<D>, grid, block, 0, stream, p);
+        hipLaunchKernelGGL((fp4_store_kernel<D, ROWS>), grid, block, 0, stream, p);
     else
-        hipLaunchKernelGGL(fp4_load_kernel<D>, grid, block, 0, stream, p);
+        hipLaunchKernelGGL((fp4_load_kernel<D, ROWS>), grid, block, 0, stream, p);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_fp4_rows(const Fp4RowParams &p, int head_dim, hipStream_t stream)
+hipError_t launch_fp4_rows(const Fp4RowParams &rows, int head_dim, hipStream_t stream)
 {
-    return head_dim == 128 ? launch<128>(p, stream) : head_dim == 64 ? launch<64>(p, stream) : hipErrorInvalidValue;
+    Fp4RowParams p = rows;
+    // exact for units below 2^32 / heads (inverse_of(1) does not fit)
+    p.heads_inverse = p.num_kv_heads > 1 && p.num_kv_heads <= 32 ? inverse_of(p.num_kv_heads) : 0;
+    const bool many = (long long)p.rows * p.num_kv_heads * head_dim >= kManyRowElements;
+    if (head_dim == 128)
+        return many ? launch<128, kRowsPerThread>(p, stream) : launch<128, 1>(p, stream);
+    if (head_dim == 64)
+        return many ? launch<64, kRowsPerThread>(p, stream) : launch<64, 1>(p, stream);
+    return hipErrorInvalidValue;
 }
 
 }  // namespace sl

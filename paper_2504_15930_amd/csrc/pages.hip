@@ -16,7 +16,7 @@ namespace {
 
 constexpr int kPageThreads = 1024;
 constexpr int kPageWaves = kPageThreads / kWave;
-constexpr int kPer = (kMaxBatch + kPageThreads - 1) / kPageThreads;   // requests per thread, at most
+constexpr int kMostPer = (kMaxBatch + kPageThreads - 1) / kPageThreads;   // requests per thread
 
 struct Sum {
     static constexpr uint32_t kIdentity = 0;
@@ -84,6 +84,7 @@ __device__ __forceinline__ uint32_t stack_size(const PageParams &p)
 }
 
 // `with_slots`: the slot map too; else fill_slots_kernel follows.
+template <int PER>
 __global__ __launch_bounds__(kPageThreads) void extend_pages_kernel(PageParams p, int with_slots)
 {
     extern __shared__ uint32_t s_dyn[];
@@ -92,15 +93,15 @@ __global__ __launch_bounds__(kPageThreads) void extend_pages_kernel(PageParams p
     uint32_t *const s_tok = s_dyn;            // [B + 1] tokens of the requests before
     uint32_t *const s_pg = s_tok + B + 1;     // [B + 1] pages that they open
     uint32_t *const s_len = s_pg + B + 1;     // [B] lengths so far
-    const int per = (B + kPageThreads - 1) / kPageThreads, first = tid * per;
+    const int per = PER == 1 ? 1 : (B + kPageThreads - 1) / kPageThreads, first = tid * per;
     const int most = p.max_blocks * kPageSize;
     const uint32_t count = stack_size(p);
-    int len[kPer];
-    uint32_t add[kPer], open[kPer];
+    int len[PER];
+    uint32_t add[PER], open[PER];
     uint32_t tok = 0, pg = 0, all_tok, all_pg;
-    bool valid[kPer];
+    bool valid[PER];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
+    for (int i = 0; i < PER; ++i) {
         const int b = first + i;
         const bool in = i < per && b < B;
         len[i] = in ? p.seq_lens[b] : 0;
@@ -116,7 +117,7 @@ __global__ __launch_bounds__(kPageThreads) void extend_pages_kernel(PageParams p
     // pages up to its own are there.
     uint32_t got_tok = 0, got_pg = 0;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
+    for (int i = 0; i < PER; ++i) {
         tok += add[i];
         pg += open[i];
         if (tok > (uint32_t)p.max_tokens || (open[i] > 0 && pg > count))
@@ -126,7 +127,7 @@ __global__ __launch_bounds__(kPageThreads) void extend_pages_kernel(PageParams p
     }
     block_sums(got_tok, got_pg, all_tok, all_pg, s_wave);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
+    for (int i = 0; i < PER; ++i) {
         const int b = first + i;
         if (i < per && b < B) {
             s_tok[b] = got_tok;
@@ -193,20 +194,21 @@ __global__ __launch_bounds__(kSlotThreads) void fill_slots_kernel(PageParams p)
     }
 }
 
+template <int PER>
 __global__ __launch_bounds__(kPageThreads) void release_pages_kernel(PageParams p)
 {
     extern __shared__ uint32_t s_dyn[];
     __shared__ uint32_t s_wave[kPageWaves][2];
     const int B = p.batch, tid = threadIdx.x;
     uint32_t *const s_pg = s_dyn;   // [B + 1] pages given back by the requests before
-    const int per = (B + kPageThreads - 1) / kPageThreads, first = tid * per;
+    const int per = PER == 1 ? 1 : (B + kPageThreads - 1) / kPageThreads, first = tid * per;
     const int most = p.max_blocks * kPageSize;
     const uint32_t count = stack_size(p);
-    int len[kPer];
-    uint32_t back[kPer];
+    int len[PER];
+    uint32_t back[PER];
     uint32_t pg = 0, none = 0, all, all_none;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
+    for (int i = 0; i < PER; ++i) {
         const int b = first + i;
         const bool in = i < per && b < B;
         len[i] = in ? p.seq_lens[b] : 0;
@@ -217,7 +219,7 @@ __global__ __launch_bounds__(kPageThreads) void release_pages_kernel(PageParams 
     }
     block_sums(pg, none, all, all_none, s_wave);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
+    for (int i = 0; i < PER; ++i) {
         const int b = first + i;
         if (i < per && b < B) {
             s_pg[b] = pg;
@@ -242,11 +244,13 @@ constexpr int kOneLaunchTokens = 4096;
 
 }  // namespace
 
+// (One request per thread where that is enough: the code for eight is four times
+// as long, and a first pass through it is instruction fetches.)
 hipError_t launch_extend_pages(const PageParams &p, hipStream_t stream)
 {
     const bool one = p.max_tokens <= kOneLaunchTokens;
-    hipLaunchKernelGGL(extend_pages_kernel, dim3(1), dim3(kPageThreads), sizeof(uint32_t) * (3 * (size_t)p.batch + 2),
-                       stream, p, one ? 1 : 0);
+    hipLaunchKernelGGL(p.batch <= kPageThreads ? extend_pages_kernel<1> : extend_pages_kernel<kMostPer>, dim3(1),
+                       dim3(kPageThreads), sizeof(uint32_t) * (3 * (size_t)p.batch + 2), stream, p, one ? 1 : 0);
     hipError_t e = hipGetLastError();
     if (one || e != hipSuccess)
         return e;
@@ -257,8 +261,8 @@ hipError_t launch_extend_pages(const PageParams &p, hipStream_t stream)
 
 hipError_t launch_release_pages(const PageParams &p, hipStream_t stream)
 {
-    hipLaunchKernelGGL(release_pages_kernel, dim3(1), dim3(kPageThreads), sizeof(uint32_t) * ((size_t)p.batch + 1),
-                       stream, p);
+    hipLaunchKernelGGL(p.batch <= kPageThreads ? release_pages_kernel<1> : release_pages_kernel<kMostPer>, dim3(1),
+                       dim3(kPageThreads), sizeof(uint32_t) * ((size_t)p.batch + 1), stream, p);
     return hipGetLastError();
 }
 

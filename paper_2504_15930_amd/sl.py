@@ -433,73 +433,71 @@ def decode_attn_prefix_fp8(q, k_pages, v_pages, k_scales, v_scales, block_table,
 
 
 # The 4-bit cache: one uint8 record of 17 D bytes per (page, KV head), as include/sl.h lays it out.
-FP4_BLOCK = 32   # elements per scale
-
 
 def fp4_record_bytes(head_dim: int) -> int:
     """Bytes of a page-head record of the 4-bit cache (16 tokens, keys and values)."""
     return 17 * head_dim
 
 
-def _need_on(index: int, t: torch.Tensor, name: str, dtype, shape):
-    """``t`` of this dtype and exact shape, contiguous, on GPU ``index``."""
+def _ptr(t: torch.Tensor, name: str, dtype, shape, index: int) -> int:
+    """Address of ``t``, which must have this dtype and exact shape, contiguous, on GPU ``index``. (One pass over
+    what decides it, 0.4 us; which of them failed is worked out only then.)"""
+    try:
+        if t.dtype is dtype and t.shape == shape and t.get_device() == index >= 0 and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
     _need(t, name, dtype, len(shape))
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.get_device() != index:
-        raise ValueError(f"{name} must be on cuda:{index} with the others")
+    raise ValueError(f"{name} must be on cuda:{index} with the others, is on {t.device}")
 
 
-def _fp4_pool(kv_pages, head_dim: int) -> tuple[int, int, int]:
-    """(GPU, num_pages, num_kv_heads) of a pool for rows of ``head_dim`` elements."""
-    _need(kv_pages, "kv_pages", torch.uint8, 3)
-    if kv_pages.shape[2] != 17 * head_dim:
-        raise ValueError(f"kv_pages must hold records of {17 * head_dim} bytes for head_dim {head_dim}, "
-                         f"got {kv_pages.shape[2]}")
-    return kv_pages.get_device(), kv_pages.shape[0], kv_pages.shape[1]
+def _shape(t: torch.Tensor, name: str, dtype, ndim: int):
+    """Shape of a tensor that names sizes (checked like the others once they are known)."""
+    if not isinstance(t, torch.Tensor) or len(t.shape) != ndim:
+        _need(t, name, dtype, ndim)
+    return t.shape
+
+
+def _record_dim(kv_pages: torch.Tensor) -> int:
+    """head_dim of a pool's records."""
+    size = _shape(kv_pages, "kv_pages", torch.uint8, 3)[2]
+    if size % 17:
+        raise ValueError(f"kv_pages must hold records of 17 D bytes, got {size}")
+    return size // 17
 
 
 def _run_fp4(q, kv_pages, block_table, seq_lens, scale, groups, out, num_workers, workspace, timing):
-    _need(q, "q", torch.bfloat16, 3)
-    B, Hq, D = q.shape
-    index, N, Hkv = _fp4_pool(kv_pages, D)
-    _need_on(index, q, "q", torch.bfloat16, q.shape)
-    _need(block_table, "block_table", torch.int32, 2)
-    _need_on(index, block_table, "block_table", torch.int32, (B, block_table.shape[1]))
-    _need_on(index, seq_lens, "seq_lens", torch.int32, (B,))
+    B, Hq, D = _shape(q, "q", torch.bfloat16, 3)
+    N, Hkv, _ = _shape(kv_pages, "kv_pages", torch.uint8, 3)
+    blocks = _shape(block_table, "block_table", torch.int32, 2)[1]
+    index = q.get_device()
+    args = [_ptr(q, "q", torch.bfloat16, (B, Hq, D), index),
+            _ptr(kv_pages, "kv_pages", torch.uint8, (N, Hkv, 17 * D), index),
+            _ptr(block_table, "block_table", torch.int32, (B, blocks), index),
+            _ptr(seq_lens, "seq_lens", torch.int32, (B,), index)]
+    sizes = (B, Hq, Hkv, D, PAGE_SIZE, blocks, N, num_workers)
+    if groups is not None:
+        ng = _shape(groups[1], "shared_pages", torch.int32, 1)[0]
+        args += [_ptr(groups[0], "group_start", torch.int32, (ng + 1,), index),
+                 _ptr(groups[1], "shared_pages", torch.int32, (ng,), index), ng]
     if out is None:
         out = torch.empty_like(q)
+        out_ptr = out.data_ptr()
     else:
-        _need_on(index, out, "out", torch.bfloat16, q.shape)
-    if groups is not None:
-        group_start, shared_pages = groups
-        _need(shared_pages, "shared_pages", torch.int32, 1)
-        ng = shared_pages.shape[0]
-        _need_on(index, shared_pages, "shared_pages", torch.int32, (ng,))
-        _need_on(index, group_start, "group_start", torch.int32, (ng + 1,))
+        out_ptr = _ptr(out, "out", torch.bfloat16, (B, Hq, D), index)
     with _device(index):
         stream = _stream(index)
-        sizes = (B, Hq, Hkv, D, PAGE_SIZE, block_table.shape[1], N, num_workers)
-        desc = make_desc(*sizes, stream)
         if B == 0:
             return out
         if workspace is None:
             workspace = _workspace(index, stream, _workspace_bytes(index, *sizes) if groups is None else
                                    _prefix_workspace_bytes(index, ng, *sizes))
-        desc.workspace = workspace.data_ptr()
-        desc.workspace_bytes = workspace.numel() * workspace.element_size()
-        if timing is not None:
-            desc.timing_start, desc.timing_stop = timing
-        lib = load()
-        if groups is None:
-            _check(lib.sl_decode_attn_fp4(ctypes.byref(desc), q.data_ptr(), kv_pages.data_ptr(),
-                                          block_table.data_ptr(), seq_lens.data_ptr(), float(scale), out.data_ptr()),
-                   "sl_decode_attn_fp4")
-        else:
-            _check(lib.sl_decode_attn_prefix_fp4(ctypes.byref(desc), q.data_ptr(), kv_pages.data_ptr(),
-                                                 block_table.data_ptr(), seq_lens.data_ptr(), group_start.data_ptr(),
-                                                 shared_pages.data_ptr(), ng, float(scale), out.data_ptr()),
-                   "sl_decode_attn_prefix_fp4")
+        desc = Desc(*sizes, stream, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                    *(timing or ()))
+        name = "sl_decode_attn_fp4" if groups is None else "sl_decode_attn_prefix_fp4"
+        _check(getattr(_lib or load(), name)(ctypes.byref(desc), *args, float(scale), out_ptr), name)
     return out
 
 
@@ -520,79 +518,56 @@ def decode_attn_prefix_fp4(q, kv_pages, block_table, seq_lens, scale, group_star
 def kv_append_fp4(k_new, v_new, block_table, seq_lens, kv_pages, *, timing=None):
     """``sl_kv_append_fp4``: a decode step's new rows [B, Hkv, D] (bf16) quantised into a 4-bit cache, in place;
     ``seq_lens`` already counts them. Asynchronous on the current stream."""
-    _need(k_new, "k_new", torch.bfloat16, 3)
-    B, Hkv, D = k_new.shape
-    index, N, heads = _fp4_pool(kv_pages, D)
-    _need_on(index, k_new, "k_new", torch.bfloat16, (B, heads, D))
-    _need_on(index, v_new, "v_new", torch.bfloat16, (B, heads, D))
-    _need(block_table, "block_table", torch.int32, 2)
-    _need_on(index, block_table, "block_table", torch.int32, (B, block_table.shape[1]))
-    _need_on(index, seq_lens, "seq_lens", torch.int32, (B,))
+    B, Hkv, D = _shape(k_new, "k_new", torch.bfloat16, 3)
+    N = _shape(kv_pages, "kv_pages", torch.uint8, 3)[0]
+    blocks = _shape(block_table, "block_table", torch.int32, 2)[1]
+    index = k_new.get_device()
+    args = (_ptr(k_new, "k_new", torch.bfloat16, (B, Hkv, D), index), _ptr(v_new, "v_new", torch.bfloat16, (B, Hkv, D), index),
+            _ptr(block_table, "block_table", torch.int32, (B, blocks), index),
+            _ptr(seq_lens, "seq_lens", torch.int32, (B,), index),
+            _ptr(kv_pages, "kv_pages", torch.uint8, (N, Hkv, 17 * D), index))
     with _device(index):
-        desc = make_desc(B, Hkv, Hkv, D, PAGE_SIZE, block_table.shape[1], N, 0, _stream(index), timing=timing)
-        _check(load().sl_kv_append_fp4(ctypes.byref(desc), k_new.data_ptr(), v_new.data_ptr(),
-                                       block_table.data_ptr(), seq_lens.data_ptr(), kv_pages.data_ptr()),
-               "sl_kv_append_fp4")
+        desc = Desc(B, Hkv, Hkv, D, PAGE_SIZE, blocks, N, 0, _stream(index), None, 0, *(timing or ()))
+        _check((_lib or load()).sl_kv_append_fp4(ctypes.byref(desc), *args), "sl_kv_append_fp4")
 
 
 def kv_write_fp4(k_new, v_new, slots, kv_pages, *, timing=None):
     """``sl_kv_write_fp4``: rows [T, Hkv, D] (bf16) quantised into the slots ``slots`` (int32 [T], page * 16 + slot in
     the page; negative: no token) of a 4-bit cache, in place. Asynchronous on the current stream."""
-    _need(k_new, "k_new", torch.bfloat16, 3)
-    T, Hkv, D = k_new.shape
-    index, N, heads = _fp4_pool(kv_pages, D)
-    _need_on(index, k_new, "k_new", torch.bfloat16, (T, heads, D))
-    _need_on(index, v_new, "v_new", torch.bfloat16, (T, heads, D))
-    _need_on(index, slots, "slots", torch.int32, (T,))
+    T, Hkv, D = _shape(k_new, "k_new", torch.bfloat16, 3)
+    N = _shape(kv_pages, "kv_pages", torch.uint8, 3)[0]
+    index = k_new.get_device()
+    args = (_ptr(k_new, "k_new", torch.bfloat16, (T, Hkv, D), index), _ptr(v_new, "v_new", torch.bfloat16, (T, Hkv, D), index),
+            _ptr(slots, "slots", torch.int32, (T,), index), T,
+            _ptr(kv_pages, "kv_pages", torch.uint8, (N, Hkv, 17 * D), index))
     with _device(index):
-        desc = make_desc(0, Hkv, Hkv, D, PAGE_SIZE, 1, N, 0, _stream(index), timing=timing)
-        _check(load().sl_kv_write_fp4(ctypes.byref(desc), k_new.data_ptr(), v_new.data_ptr(), slots.data_ptr(), T,
-                                      kv_pages.data_ptr()), "sl_kv_write_fp4")
+        desc = Desc(0, Hkv, Hkv, D, PAGE_SIZE, 1, N, 0, _stream(index), None, 0, *(timing or ()))
+        _check((_lib or load()).sl_kv_write_fp4(ctypes.byref(desc), *args), "sl_kv_write_fp4")
 
 
 def kv_read_fp4(slots, kv_pages, *, k_out=None, v_out=None, timing=None) -> tuple[torch.Tensor, torch.Tensor]:
     """``sl_kv_read_fp4``: the key and value rows (bf16 [T, Hkv, D]) in the slots ``slots`` (int32 [T]) of a 4-bit
     cache; zero rows for negative slots, NaN for slots past the pool. Asynchronous on the current stream."""
-    _need(kv_pages, "kv_pages", torch.uint8, 3)
-    if kv_pages.shape[2] % 17:
-        raise ValueError(f"kv_pages must hold records of 17 D bytes, got {kv_pages.shape[2]}")
-    D = kv_pages.shape[2] // 17
-    index, N, Hkv = _fp4_pool(kv_pages, D)
-    _need(slots, "slots", torch.int32, 1)
-    T = slots.shape[0]
-    _need_on(index, slots, "slots", torch.int32, (T,))
-    rows = []
-    for t, name in ((k_out, "k_out"), (v_out, "v_out")):
-        if t is None:
-            t = torch.empty((T, Hkv, D), dtype=torch.bfloat16, device=kv_pages.device)
-        else:
-            _need_on(index, t, name, torch.bfloat16, (T, Hkv, D))
-        rows.append(t)
+    D = _record_dim(kv_pages)
+    N, Hkv, _ = kv_pages.shape
+    T = _shape(slots, "slots", torch.int32, 1)[0]
+    index = kv_pages.get_device()
+    pool = _ptr(kv_pages, "kv_pages", torch.uint8, (N, Hkv, 17 * D), index)
+    at = _ptr(slots, "slots", torch.int32, (T,), index)
+    if k_out is None:
+        k_out = torch.empty((T, Hkv, D), dtype=torch.bfloat16, device=kv_pages.device)
+        k_ptr = k_out.data_ptr()
+    else:
+        k_ptr = _ptr(k_out, "k_out", torch.bfloat16, (T, Hkv, D), index)
+    if v_out is None:
+        v_out = torch.empty((T, Hkv, D), dtype=torch.bfloat16, device=kv_pages.device)
+        v_ptr = v_out.data_ptr()
+    else:
+        v_ptr = _ptr(v_out, "v_out", torch.bfloat16, (T, Hkv, D), index)
     with _device(index):
-        desc = make_desc(0, Hkv, Hkv, D, PAGE_SIZE, 1, N, 0, _stream(index), timing=timing)
-        _check(load().sl_kv_read_fp4(ctypes.byref(desc), kv_pages.data_ptr(), slots.data_ptr(), T,
-                                     rows[0].data_ptr(), rows[1].data_ptr()), "sl_kv_read_fp4")
-    return rows[0], rows[1]
-
-
-def _pages_args(seq_lens, marks, marks_name, block_table, free_pages, free_count, seq_lens_out, free_count_out):
-    """Checks common to the page bookkeeping; returns (GPU, batch, max_blocks, num_pages, the two outputs)."""
-    _need(seq_lens, "seq_lens", torch.int32, 1)
-    _need(block_table, "block_table", torch.int32, 2)
-    _need(free_pages, "free_pages", torch.int32, 1)
-    index, B, blocks, N = seq_lens.get_device(), seq_lens.shape[0], block_table.shape[1], free_pages.shape[0]
-    _need_on(index, marks, marks_name, torch.int32, (B,))
-    _need_on(index, block_table, "block_table", torch.int32, (B, blocks))
-    _need_on(index, free_pages, "free_pages", torch.int32, (N,))
-    _need_on(index, free_count, "free_count", torch.int32, (1,))
-    outs = []
-    for t, name, like in ((seq_lens_out, "seq_lens_out", seq_lens), (free_count_out, "free_count_out", free_count)):
-        if t is None:
-            t = torch.empty_like(like)
-        else:
-            _need_on(index, t, name, torch.int32, like.shape)
-        outs.append(t)
-    return index, B, blocks, N, outs
+        desc = Desc(0, Hkv, Hkv, D, PAGE_SIZE, 1, N, 0, _stream(index), None, 0, *(timing or ()))
+        _check((_lib or load()).sl_kv_read_fp4(ctypes.byref(desc), pool, at, T, k_ptr, v_ptr), "sl_kv_read_fp4")
+    return k_out, v_out
 
 
 def pages_extend(seq_lens, new_tokens, block_table, free_pages, free_count, max_tokens, *, seq_lens_out=None,
@@ -602,33 +577,52 @@ def pages_extend(seq_lens, new_tokens, block_table, free_pages, free_count, max_
     place. Returns ``(seq_lens_out, token_start, slots, free_count_out)``: the new lengths [B], where each request's
     tokens begin in the slot map [B + 1], the slot map [max_tokens] (-1 past the last token), and the pages left.
     ``seq_lens_out`` and ``free_count_out`` may be the inputs themselves. All int32; asynchronous."""
-    index, B, blocks, N, (lens, count) = _pages_args(seq_lens, new_tokens, "new_tokens", block_table, free_pages,
-                                                     free_count, seq_lens_out, free_count_out)
-    if token_start is None:
-        token_start = torch.empty(B + 1, dtype=torch.int32, device=seq_lens.device)
+    B = _shape(seq_lens, "seq_lens", torch.int32, 1)[0]
+    blocks = _shape(block_table, "block_table", torch.int32, 2)[1]
+    N = _shape(free_pages, "free_pages", torch.int32, 1)[0]
+    index = seq_lens.get_device()
+    args = (_ptr(seq_lens, "seq_lens", torch.int32, (B,), index), _ptr(new_tokens, "new_tokens", torch.int32, (B,), index),
+            _ptr(block_table, "block_table", torch.int32, (B, blocks), index),
+            _ptr(free_pages, "free_pages", torch.int32, (N,), index),
+            _ptr(free_count, "free_count", torch.int32, (1,), index), max_tokens)
+    if seq_lens_out is None and free_count_out is None and token_start is None and slots is None:
+        # one allocation for all four
+        room = torch.empty(2 * B + 2 + max_tokens, dtype=torch.int32, device=seq_lens.device)
+        at = room.data_ptr()
+        args += (at, at + 4 * (2 * B + 1 + max_tokens), at + 4 * B, at + 4 * (2 * B + 1))
+        seq_lens_out, token_start, slots, free_count_out = room.split((B, B + 1, max_tokens, 1))
     else:
-        _need_on(index, token_start, "token_start", torch.int32, (B + 1,))
-    if slots is None:
-        slots = torch.empty(max_tokens, dtype=torch.int32, device=seq_lens.device)
-    else:
-        _need_on(index, slots, "slots", torch.int32, (max_tokens,))
+        new = lambda t, n: torch.empty(n, dtype=torch.int32, device=seq_lens.device) if t is None else t
+        seq_lens_out, free_count_out = new(seq_lens_out, B), new(free_count_out, 1)
+        token_start, slots = new(token_start, B + 1), new(slots, max_tokens)
+        args += (_ptr(seq_lens_out, "seq_lens_out", torch.int32, (B,), index),
+                 _ptr(free_count_out, "free_count_out", torch.int32, (1,), index),
+                 _ptr(token_start, "token_start", torch.int32, (B + 1,), index),
+                 _ptr(slots, "slots", torch.int32, (max_tokens,), index))
     with _device(index):
-        desc = make_desc(B, 1, 1, 64, PAGE_SIZE, blocks, N, 0, _stream(index))
-        _check(load().sl_pages_extend(ctypes.byref(desc), seq_lens.data_ptr(), new_tokens.data_ptr(),
-                                      block_table.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(),
-                                      max_tokens, lens.data_ptr(), count.data_ptr(), token_start.data_ptr(),
-                                      slots.data_ptr()), "sl_pages_extend")
-    return lens, token_start, slots, count
+        desc = Desc(B, 1, 1, 64, PAGE_SIZE, blocks, N, 0, _stream(index))
+        _check((_lib or load()).sl_pages_extend(ctypes.byref(desc), *args), "sl_pages_extend")
+    return seq_lens_out, token_start, slots, free_count_out
 
 
 def pages_release(finished, seq_lens, block_table, free_pages, free_count, *, seq_lens_out=None, free_count_out=None):
     """``sl_pages_release``: the pages of requests with ``finished`` [B] not 0 go back on the stack, in place, and
     their lengths become 0. Returns ``(seq_lens_out, free_count_out)``, which may be the inputs themselves."""
-    index, B, blocks, N, (lens, count) = _pages_args(seq_lens, finished, "finished", block_table, free_pages,
-                                                     free_count, seq_lens_out, free_count_out)
+    B = _shape(seq_lens, "seq_lens", torch.int32, 1)[0]
+    blocks = _shape(block_table, "block_table", torch.int32, 2)[1]
+    N = _shape(free_pages, "free_pages", torch.int32, 1)[0]
+    index = seq_lens.get_device()
+    args = (_ptr(finished, "finished", torch.int32, (B,), index), _ptr(seq_lens, "seq_lens", torch.int32, (B,), index),
+            _ptr(block_table, "block_table", torch.int32, (B, blocks), index),
+            _ptr(free_pages, "free_pages", torch.int32, (N,), index),
+            _ptr(free_count, "free_count", torch.int32, (1,), index))
+    if seq_lens_out is None:
+        seq_lens_out = torch.empty_like(seq_lens)
+    if free_count_out is None:
+        free_count_out = torch.empty_like(free_count)
+    args += (_ptr(seq_lens_out, "seq_lens_out", torch.int32, (B,), index),
+             _ptr(free_count_out, "free_count_out", torch.int32, (1,), index))
     with _device(index):
-        desc = make_desc(B, 1, 1, 64, PAGE_SIZE, blocks, N, 0, _stream(index))
-        _check(load().sl_pages_release(ctypes.byref(desc), finished.data_ptr(), seq_lens.data_ptr(),
-                                       block_table.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(),
-                                       lens.data_ptr(), count.data_ptr()), "sl_pages_release")
-    return lens, count
+        desc = Desc(B, 1, 1, 64, PAGE_SIZE, blocks, N, 0, _stream(index))
+        _check((_lib or load()).sl_pages_release(ctypes.byref(desc), *args), "sl_pages_release")
+    return seq_lens_out, free_count_out
