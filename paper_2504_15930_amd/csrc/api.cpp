@@ -46,7 +46,7 @@ size_t prefix_workspace_layout(void *base, int batch, int max_blocks, int num_kv
     w.cum_own = reinterpret_cast<int32_t *>(take(sizeof(int32_t) * ((size_t)batch + 1)));
     w.seq_shared = reinterpret_cast<int32_t *>(take(sizeof(int32_t) * 4 * (size_t)batch));
     w.cum_shared = reinterpret_cast<int32_t *>(
-        take(sizeof(int32_t) * ((size_t)prefix_max_sub(batch, num_groups, group) + 1)));
+        take(sizeof(int32_t) * ((size_t)prefix_max_sub(batch, num_groups, group) + 2)));
     w.own_ml = reinterpret_cast<float *>(take(sizeof(float) * 2 * (size_t)num_workers * group * 2));
     w.own_acc = reinterpret_cast<float *>(take(sizeof(float) * 2 * (size_t)num_workers * group * head_dim));
     w.shared_ml = reinterpret_cast<float *>(take(sizeof(float) * 2 * (size_t)num_workers * kPrefixRows * 2));

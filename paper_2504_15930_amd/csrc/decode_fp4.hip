@@ -18,6 +18,23 @@ __global__ __launch_bounds__(kWave * kWavesPerBlock) void split_fp4_kernel(Split
     split_unit_worker<D, KV, kAllPages>(p, wave * (int)gridDim.x + (int)blockIdx.x, StreamLds{s_cum, s_len});
 }
 
+// Shared-page workers per workgroup: 4, 2 or 1 for units of up to 16, 32 and 64
+// query rows (members x heads of the largest sub-group with shared pages). With
+// four wavefronts per worker whatever the rows, those of the empty blocks stream
+// and compute for nothing: 8 prompts of 4000 tokens x 2 samples, 32/8 heads, D = 64
+// 31.8 -> 23.6 us; 16 of 4000 x 24, 12/12 heads, D = 64 115 -> 51; 64 of 2000 x 4,
+// 64/8 heads, D = 128 118 -> 79; with four blocks the same.
+// (Every wavefront looks for itself: two votes of the workgroup took 1 us.)
+__device__ __forceinline__ int shared_workers_per_block(const int32_t *s_sh, const int32_t *s_gl, int S, int group)
+{
+    int members = 0;
+    for (int i = threadIdx.x & (kWave - 1); i < S; i += kWave)
+        if (s_sh[i + 1] > s_sh[i])
+            members = max(members, (s_gl[i] >> 16 & 15) + 1);
+    const int rows = wave_reduce<ScanMax>(members) * group;
+    return rows > 32 ? 1 : rows > 16 ? 2 : 4;
+}
+
 template <int D, int KV>
 __global__ __launch_bounds__(kWave * kWavesPerBlock) void prefix_fp4_kernel(SplitParams own, SplitParams shared,
                                                                                PrefixParams pp, int own_blocks,
@@ -36,17 +53,26 @@ __global__ __launch_bounds__(kWave * kWavesPerBlock) void prefix_fp4_kernel(Spli
     int32_t *const s_sp = s_gs + pp.num_groups + 1;                         // [NG]
     constexpr int NT = step_tiles<D, KV, true>();
     scan_prefix_groups<NT>(own, pp, s_own, s_len, s_shared, s_sh, s_gl, s_gs, s_sp);
+    const int per_block = shared_workers_per_block(s_sh, s_gl, S, own.group);
+    if (blockIdx.x == 0 && threadIdx.x == 0)
+        pp.cum_shared[S + 1] = per_block;
     if ((int)blockIdx.x < own_blocks)
         split_unit_worker<D, KV, kOwnPages>(
             own, blockIdx.x * kWavesPerBlock + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave),
             StreamLds{s_own, s_len, s_shared});
     else {
+        // The four wavefronts of a workgroup are one worker (four column blocks of
+        // query rows), or two or four where the largest unit has two blocks or one.
+        const int block = (int)blockIdx.x - own_blocks;
+        const int blocks = effective_shared_workers((long long)s_own[B] * own.num_kv_heads, own.num_workers,
+                                                    shared.num_workers, max_shared, NT, kFp4);
+        if (block >= blocks)
+            return;
         SplitParams sh = shared;
-        sh.num_workers = effective_shared_workers((long long)s_own[B] * own.num_kv_heads, own.num_workers,
-                                                  shared.num_workers, max_shared, NT, kFp4);
-        split_unit_worker<D, kFp4, kSharedPages>(sh, (int)blockIdx.x - own_blocks,
-                                                  StreamLds{s_sh, nullptr, nullptr, s_gl, S},
-                                                  __builtin_amdgcn_readfirstlane(threadIdx.x / kWave));
+        sh.num_workers = shared_workers_of(blocks, per_block, own.num_workers);
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), waves = kPrefixBlocks / per_block;
+        split_unit_worker<D, kFp4, kSharedPages>(sh, wave / waves * blocks + block,
+                                                 StreamLds{s_sh, nullptr, nullptr, s_gl, S}, wave % waves);
     }
 }
 

@@ -71,14 +71,14 @@ namespace {
 //   E4M3 D = 64, 384 x 1..4096 tokens, 8 KV heads   226 -> 146 us (two tiles: 157)
 // FP4: four tiles per step carry as much as two of E4M3 (two per step: 512 x 512 +
 // lognormal(2048), 28/4 heads, 191 us instead of 172), but not in the prefix
-// kernel, where the registers of four leave no room for a shared-page workgroup
-// beside an own-page one (32 prompts x 8 samples, 59 us instead of 43).
+// kernel of D = 128, where the registers of four leave no room for a shared-page
+// workgroup beside an own-page one (32 prompts x 8 samples, 59 us instead of 43).
 // Two steps in flight; three were no faster anywhere (and slower where they
 // cost a resident workgroup, in the prefix kernel).
 template <int D, int KV, bool PREFIX = false>
 constexpr int step_tiles()
 {
-    return is_fp4(KV) ? (PREFIX ? 2 : 4) : D == 64 ? (KV == kE4m3 ? 4 : 2) : (KV == kE4m3 ? 2 : 1);
+    return is_fp4(KV) ? (PREFIX && D == 128 ? 2 : 4) : D == 64 ? (KV == kE4m3 ? 4 : 2) : (KV == kE4m3 ? 2 : 1);
 }
 constexpr int kPipelineDepth = 2;
 // Four E4M3 codes (one dword) -> four bf16 (two dwords), exact.
@@ -824,7 +824,8 @@ struct StreamLds {
 // Worker w of the split-KV pass over the stream that `sv` describes (in LDS,
 // complete: the caller has passed a barrier). A worker is one wavefront, or
 // for kSharedPages the four wavefronts of a workgroup, which stream the same
-// tiles and compute column blocks blk = 0..3 of each shared unit.
+// tiles and compute column blocks blk = 0..3 of each shared unit (FP4: as many
+// wavefronts as the units have blocks, one, two or four).
 template <int D, int KV, int MODE>
 __device__ __forceinline__ void split_unit_worker(const SplitParams &p, int w, const StreamLds &sv, int blk = -1)
 {

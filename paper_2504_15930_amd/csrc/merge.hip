@@ -238,6 +238,7 @@ __global__ __launch_bounds__(kMergeThreads) void merge_prefix_kernel(PrefixMerge
     const int ob = p.cum_own[b + 1] - co;
     const long long tot_o = (long long)p.cum_own[p.batch] * Hkv;
     const long long tot_s = (long long)p.cum_shared[p.max_sub] * Hkv;
+    const int per_block = p.kv == kFp4 ? p.cum_shared[p.max_sub + 1] : 1;   // shared-page workers
     const bool bad = L < 0 || L > p.max_blocks * kPageSize || L < sk * kPageSize;
     if (sk == 0 && ob == 0) {
         const uint32_t fill = L < 0 ? 0x7fc07fc0u : 0u;   // bf16 NaN / +0
@@ -246,10 +247,12 @@ __global__ __launch_bounds__(kMergeThreads) void merge_prefix_kernel(PrefixMerge
         return;
     }
     const int nw_o = effective_workers(tot_o, p.num_workers, p.step_tiles, wide_from(p.num_workers, p.kv));
-    const int nw_s = effective_workers(tot_s,
-                                       effective_shared_workers(tot_o, p.num_workers, p.num_shared_workers,
-                                                                p.max_shared_workers, p.step_tiles, p.kv),
-                                       p.step_tiles, 0);
+    const int nw_s = effective_workers(
+        tot_s,
+        shared_workers_of(effective_shared_workers(tot_o, p.num_workers, p.num_shared_workers, p.max_shared_workers,
+                                                   p.step_tiles, p.kv),
+                          per_block, p.num_workers),
+        p.step_tiles, 0);
     const long long a_o = (long long)Hkv * co + (long long)g * ob;
     const long long a_s = (long long)Hkv * s_start + (long long)g * ss;
     const Cuts cuts = cuts_of(a_s, ss, tot_s, nw_s, a_o, ob, tot_o, nw_o, lane);   // (an empty unit's is not used)

@@ -139,6 +139,15 @@ constexpr uint32_t kMetaPrefixed = 1u << 7;   // own-page unit of a sequence who
 // blocks of 16).
 constexpr int kPrefixBlocks = 4;
 constexpr int kPrefixRows = 16 * kPrefixBlocks;
+// FP4: a shared-page worker is only as many wavefronts as the call's largest
+// shared unit has column blocks (1, 2 or 4: kPrefixBlocks / per_block), and a
+// workgroup holds `per_block` workers; `blocks` workgroups, and partial-state slots
+// for num_workers.
+__host__ __device__ inline int shared_workers_of(int blocks, int per_block, int num_workers)
+{
+    const int n = blocks * per_block;
+    return per_block > 1 && n > num_workers ? num_workers : n;
+}
 constexpr int kMetaUnitShift = 8;
 
 struct Workspace {
@@ -183,7 +192,8 @@ struct PrefixParams {
     const int32_t *group_start;   // [num_groups + 1]
     const int32_t *shared_pages;  // [num_groups]
     int32_t *cum_own;             // [B + 1] prefix sum of steps over own (unshared) pages
-    int32_t *cum_shared;          // [max_sub + 1] prefix sum of steps over shared pages per sub-group
+    int32_t *cum_shared;          // [max_sub + 1] prefix sum of steps over shared pages per sub-group, and
+                                  // behind it, FP4 only, the shared-page workers per workgroup
     int32_t *seq_shared;          // [B][4] per sequence: first shared step of its sub-group in the shared
                                   // stream, shared pages, sub-group's first member, shared steps (zeros if
                                   // unshared)
