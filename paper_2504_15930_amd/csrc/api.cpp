@@ -166,6 +166,27 @@ sl_status resolve_workers(const sl_attn_desc *d, int kv, int *nw, bool prefix = 
 // slots are sized.
 int shared_workers(int nw) { return nw / 4 > 0 ? nw / 4 : 1; }
 
+// Wavefronts per unit if plain attention over a 4-bit cache runs as one workgroup
+// per unit (launch_unit_fp4), else 0: where the block table says that every
+// sequence is short. (The lengths themselves are not known here; a call with a
+// worker count of its own gets the workers.) Eight where that leaves every
+// workgroup a CU. Calls, split and merge -> a workgroup per unit, MI355X, tokens
+// 1 .. 16 times the table's blocks:
+//   blocks                 16             64            128               256
+//   5 x 28/4 heads                   13.0 ->  9.5   13.0 ->  9.7
+//   64 x 28/4          13.2 ->  9.5  15.3 ->  9.4   17.3 -> 12.0   22.0 -> 19.0
+//   256 x 28/4                       20.6 -> 12.1   34.2 -> 29.4   56.3 -> 58.7
+//   512 x 64/8         37.1 -> 26.0  71.4 -> 57.2
+//   384 x 32/8, D = 64 19.6 -> 13.6  35.6 -> 26.4   52.3 -> 44.9   90.5 -> 87.0
+//   4 x 32/8, D = 64                                               13.0 -> 14.5
+// (512 x 64/8 of 16 blocks with eight wavefronts 42.6, 64 x 28/4 of 128 with four 13.4.)
+int unit_waves(const sl_attn_desc *d, int kv)
+{
+    if (kv != kFp4 || d->num_workers != 0 || d->max_blocks_per_seq > kUnitBlocks)
+        return 0;
+    return (long long)d->batch * d->num_kv_heads <= 256 ? 8 : 4;
+}
+
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
@@ -226,6 +247,12 @@ sl_status run(const sl_attn_desc *d, const uint16_t *q, const void *k_pages, con
     sp.num_pages = d->num_pages;
     if (d->timing_start && hipEventRecord(d->timing_start, d->stream) != hipSuccess)
         return SL_ERR_HIP;
+    if (const int waves = unit_waves(d, kv)) {
+        if (launch_unit_fp4(sp, waves, d->head_dim, d->stream) != hipSuccess ||
+            (d->timing_stop && hipEventRecord(d->timing_stop, d->stream) != hipSuccess))
+            return SL_ERR_HIP;
+        return SL_OK;
+    }
     if (launch_split(sp, d->head_dim, kv, d->stream) != hipSuccess)
         return SL_ERR_HIP;
     if (d->timing_stop && hipEventRecord(d->timing_stop, d->stream) != hipSuccess)

@@ -76,7 +76,124 @@ __global__ __launch_bounds__(kWave * kWavesPerBlock) void prefix_fp4_kernel(Spli
     }
 }
 
+// Plain attention where every sequence is short (a block table of at most
+// kUnitBlocks entries): one workgroup per unit, its tiles dealt to the wavefronts
+// in contiguous runs of whole steps, their states combined in LDS. One launch, no
+// scan of the batch, no partial states in memory, two trips to memory before the
+// first product (length and table entries, then records and query rows). Bound by
+// that latency, and with thousands of units by instructions, as the stream is.
+// Steps of two tiles: with four, fewer workgroups fit a CU (384 x 1..1024, 32/8
+// heads, D = 64 29.6 us instead of 26.4; 512 x 1..256, 64/8 heads 40.5 and 26.0).
+template <int D, int KV, int WAVES>
+__global__ __launch_bounds__(kWave * WAVES) void unit_fp4_kernel(SplitParams p)
+{
+    constexpr int NT = kUnitStepTiles;
+    constexpr bool HALF = KV == kFp4Half;
+    // Per wavefront what stage_partial writes: G rows of D fp32, then G pairs (m, l).
+    __shared__ __attribute__((aligned(16))) uint8_t s_state[WAVES][(HALF ? 8 : kMaxGroup) * (D + 2) * 4];
+    const int G = p.group, Hkv = p.num_kv_heads;
+    const int unit = blockIdx.x, b = unit / Hkv, g = unit - b * Hkv;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x & (kWave - 1);
+    const int n = lane & 15, quad = lane >> 4;
+    const int max_len = p.max_blocks * kPageSize;
+    const int L = p.seq_lens[b];
+    const int pages = pages_of(L, max_len), steps = (pages + NT - 1) / NT;
+    const int first = wave * steps / WAVES, count = (wave + 1) * steps / WAVES - first;
+    const int tiles = min(count * NT, pages - first * NT);   // this wavefront's, at most kWave
+    static_assert(kUnitBlocks <= WAVES * kWave, "a run's addresses lie in the lanes");
+    // Lane i: the address of tile i of the run (those past it: the last one's).
+    const int page = p.block_table[(size_t)b * p.max_blocks + max(0, min(first * NT + min(lane, tiles - 1), pages - 1))];
+    const bool in = page >= 0 && page < p.num_pages;
+    const bool bad = L < 0 || L > max_len || __builtin_amdgcn_ballot_w64(lane < tiles && !in) != 0;
+    const uint64_t record = reinterpret_cast<uint64_t>(p.k_pages) +
+                            (in ? (uint64_t)(uint32_t)(page * Hkv + g) * (uint32_t)fp4_record_bytes(D) : 0u);
+    u32x4_t q[D / 32];
+    load_q<D, KV>(q, p, (uint32_t)unit * (uint32_t)G, true, HALF ? n & 7 : n, quad);
+    Fp4Tile<D> buf[2][NT];
+    auto issue = [&](Fp4Tile<D>(&t)[NT], int i) {
+#pragma unroll
+        for (int u = 0; u < NT; ++u) {
+            const int at = max(0, min(i * NT + u, tiles - 1));
+            const uint64_t address = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)record, at) |
+                                     (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(record >> 32), at) << 32;
+            issue_record<D, kCachePolicyStream>(t[u], address, i < count, n, quad, lane);
+        }
+    };
+    issue(buf[0], 0);
+    Fp4State<D, HALF> state;
+    reset(state);
+    bf16x8_t qop[D / 32];
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s)
+        qop[s] = __builtin_bit_cast(bf16x8_t, q[s] ^ fp4_sign(p.scale_log2));
+    const float mul = __builtin_fabsf(p.scale_log2);
+    for (int i0 = 0; i0 < count; i0 += 2) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int i = i0 + k;
+            issue(buf[1 - k], i + 1);
+            if (i < count)
+                fp4_step<D, NT>(state, buf[k], qop, mul, min(kPageSize * NT, L - kPageSize * NT * (first + i)), n,
+                                quad);
+        }
+    }
+    {
+        const Piece<D> st = finished(state, quad);
+        const float l = quad_sum(st.l);
+        if (n < G)
+            stage_partial<D>(st, l, bad, s_state[wave], G, n, quad);
+    }
+    __syncthreads();
+    // out = sum of 2^(m_w - M) acc_w / sum of 2^(m_w - M) l_w; a weight of zero drops its state.
+    for (int i = threadIdx.x; i < G * (D / 4); i += kWave * WAVES) {
+        const int row = i / (D / 4), c4 = 4 * (i % (D / 4));
+        f32x2_t ml[WAVES];
+        float M = kNegInf;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            ml[w] = *reinterpret_cast<const f32x2_t *>(s_state[w] + (size_t)G * D * 4 + 8 * row);
+            M = fmaxf(M, ml[w][0]);
+        }
+        f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+        float l = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float c = __builtin_amdgcn_exp2f(ml[w][0] - M);
+            if (c != 0.0f) {
+                acc += c * *reinterpret_cast<const f32x4_t *>(s_state[w] + ((size_t)row * D + c4) * 4);
+                l += c * ml[w][1];
+            }
+        }
+        const float inv = pages == 0 ? (L < 0 ? __builtin_nanf("") : 0.0f) : 1.0f / l;
+        if (pages == 0)
+            acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        *reinterpret_cast<u32x2_t *>(p.out + ((size_t)unit * G + row) * D + c4) =
+            u32x2_t{pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv)};
+    }
+}
+
 }  // namespace
+
+namespace {
+template <int WAVES>
+SplitKernel unit_kernel(int head_dim, int group)
+{
+    if (head_dim == 128)
+        return group <= 8 ? unit_fp4_kernel<128, kFp4Half, WAVES> : unit_fp4_kernel<128, kFp4, WAVES>;
+    if (head_dim == 64)
+        return group <= 8 ? unit_fp4_kernel<64, kFp4Half, WAVES> : unit_fp4_kernel<64, kFp4, WAVES>;
+    return nullptr;
+}
+}  // namespace
+
+hipError_t launch_unit_fp4(const SplitParams &p, int waves, int head_dim, hipStream_t stream)
+{
+    const SplitKernel kernel = waves == 8 ? unit_kernel<8>(head_dim, p.group) : unit_kernel<4>(head_dim, p.group);
+    if (!kernel)
+        return hipErrorInvalidValue;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.batch * p.num_kv_heads)), dim3(kWave * waves), 0, stream, p);
+    return hipGetLastError();
+}
 
 SplitKernel split_fp4_kernel_of(int head_dim, int group)
 {

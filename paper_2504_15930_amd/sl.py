@@ -453,51 +453,49 @@ def _ptr(t: torch.Tensor, name: str, dtype, shape, index: int) -> int:
     raise ValueError(f"{name} must be on cuda:{index} with the others, is on {t.device}")
 
 
-def _shape(t: torch.Tensor, name: str, dtype, ndim: int):
-    """Shape of a tensor that names sizes (checked like the others once they are known)."""
-    if not isinstance(t, torch.Tensor) or len(t.shape) != ndim:
-        _need(t, name, dtype, ndim)
-    return t.shape
+def _refuse(*args):
+    """Raise for whichever of the (tensor, name, dtype, dims) is not what it must be."""
+    for a in args:
+        _need(*a)
+    raise ValueError("the arguments disagree on shape")
 
 
-def _record_dim(kv_pages: torch.Tensor) -> int:
-    """head_dim of a pool's records."""
-    size = _shape(kv_pages, "kv_pages", torch.uint8, 3)[2]
-    if size % 17:
-        raise ValueError(f"kv_pages must hold records of 17 D bytes, got {size}")
-    return size // 17
+_BAD_SIZES = (AttributeError, IndexError, TypeError, ValueError)   # what asking a wrong argument for its sizes raises
 
 
 def _run_fp4(q, kv_pages, block_table, seq_lens, scale, groups, out, num_workers, workspace, timing):
-    B, Hq, D = _shape(q, "q", torch.bfloat16, 3)
-    N, Hkv, _ = _shape(kv_pages, "kv_pages", torch.uint8, 3)
-    blocks = _shape(block_table, "block_table", torch.int32, 2)[1]
-    index = q.get_device()
+    try:
+        (B, Hq, D), (N, Hkv, _), (_, blocks), index = q.shape, kv_pages.shape, block_table.shape, q.get_device()
+        ng = 0 if groups is None else groups[1].shape[0]
+    except _BAD_SIZES:
+        _refuse((q, "q", torch.bfloat16, 3), (kv_pages, "kv_pages", torch.uint8, 3),
+                (block_table, "block_table", torch.int32, 2),
+                *(((groups[1], "shared_pages", torch.int32, 1),) if groups is not None else ()))
     args = [_ptr(q, "q", torch.bfloat16, (B, Hq, D), index),
             _ptr(kv_pages, "kv_pages", torch.uint8, (N, Hkv, 17 * D), index),
             _ptr(block_table, "block_table", torch.int32, (B, blocks), index),
             _ptr(seq_lens, "seq_lens", torch.int32, (B,), index)]
     sizes = (B, Hq, Hkv, D, PAGE_SIZE, blocks, N, num_workers)
     if groups is not None:
-        ng = _shape(groups[1], "shared_pages", torch.int32, 1)[0]
         args += [_ptr(groups[0], "group_start", torch.int32, (ng + 1,), index),
                  _ptr(groups[1], "shared_pages", torch.int32, (ng,), index), ng]
+    if torch._C._cuda_getDevice() != index:
+        with torch.cuda.device(index):
+            return _run_fp4(q, kv_pages, block_table, seq_lens, scale, groups, out, num_workers, workspace, timing)
     if out is None:
         out = torch.empty_like(q)
         out_ptr = out.data_ptr()
     else:
         out_ptr = _ptr(out, "out", torch.bfloat16, (B, Hq, D), index)
-    with _device(index):
-        stream = _stream(index)
-        if B == 0:
-            return out
-        if workspace is None:
-            workspace = _workspace(index, stream, _workspace_bytes(index, *sizes) if groups is None else
-                                   _prefix_workspace_bytes(index, ng, *sizes))
-        desc = Desc(*sizes, stream, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                    *(timing or ()))
-        name = "sl_decode_attn_fp4" if groups is None else "sl_decode_attn_prefix_fp4"
-        _check(getattr(_lib or load(), name)(ctypes.byref(desc), *args, float(scale), out_ptr), name)
+    if B == 0:
+        return out
+    stream = _stream(index)
+    if workspace is None:
+        workspace = _workspace(index, stream, _workspace_bytes(index, *sizes) if groups is None else
+                               _prefix_workspace_bytes(index, ng, *sizes))
+    desc = Desc(*sizes, stream, workspace.data_ptr(), workspace.numel() * workspace.element_size(), *(timing or ()))
+    name = "sl_decode_attn_fp4" if groups is None else "sl_decode_attn_prefix_fp4"
+    _check(getattr(_lib or load(), name)(ctypes.byref(desc), *args, float(scale), out_ptr), name)
     return out
 
 
@@ -518,55 +516,64 @@ def decode_attn_prefix_fp4(q, kv_pages, block_table, seq_lens, scale, group_star
 def kv_append_fp4(k_new, v_new, block_table, seq_lens, kv_pages, *, timing=None):
     """``sl_kv_append_fp4``: a decode step's new rows [B, Hkv, D] (bf16) quantised into a 4-bit cache, in place;
     ``seq_lens`` already counts them. Asynchronous on the current stream."""
-    B, Hkv, D = _shape(k_new, "k_new", torch.bfloat16, 3)
-    N = _shape(kv_pages, "kv_pages", torch.uint8, 3)[0]
-    blocks = _shape(block_table, "block_table", torch.int32, 2)[1]
-    index = k_new.get_device()
+    try:
+        (B, Hkv, D), N, blocks, index = k_new.shape, kv_pages.shape[0], block_table.shape[1], k_new.get_device()
+    except _BAD_SIZES:
+        _refuse((k_new, "k_new", torch.bfloat16, 3), (kv_pages, "kv_pages", torch.uint8, 3),
+                (block_table, "block_table", torch.int32, 2))
     args = (_ptr(k_new, "k_new", torch.bfloat16, (B, Hkv, D), index), _ptr(v_new, "v_new", torch.bfloat16, (B, Hkv, D), index),
             _ptr(block_table, "block_table", torch.int32, (B, blocks), index),
             _ptr(seq_lens, "seq_lens", torch.int32, (B,), index),
             _ptr(kv_pages, "kv_pages", torch.uint8, (N, Hkv, 17 * D), index))
-    with _device(index):
-        desc = Desc(B, Hkv, Hkv, D, PAGE_SIZE, blocks, N, 0, _stream(index), None, 0, *(timing or ()))
-        _check((_lib or load()).sl_kv_append_fp4(ctypes.byref(desc), *args), "sl_kv_append_fp4")
+    if torch._C._cuda_getDevice() != index:
+        with torch.cuda.device(index):
+            return kv_append_fp4(k_new, v_new, block_table, seq_lens, kv_pages, timing=timing)
+    desc = Desc(B, Hkv, Hkv, D, PAGE_SIZE, blocks, N, 0, _stream(index), None, 0, *(timing or ()))
+    _check((_lib or load()).sl_kv_append_fp4(ctypes.byref(desc), *args), "sl_kv_append_fp4")
 
 
 def kv_write_fp4(k_new, v_new, slots, kv_pages, *, timing=None):
     """``sl_kv_write_fp4``: rows [T, Hkv, D] (bf16) quantised into the slots ``slots`` (int32 [T], page * 16 + slot in
     the page; negative: no token) of a 4-bit cache, in place. Asynchronous on the current stream."""
-    T, Hkv, D = _shape(k_new, "k_new", torch.bfloat16, 3)
-    N = _shape(kv_pages, "kv_pages", torch.uint8, 3)[0]
-    index = k_new.get_device()
+    try:
+        (T, Hkv, D), N, index = k_new.shape, kv_pages.shape[0], k_new.get_device()
+    except _BAD_SIZES:
+        _refuse((k_new, "k_new", torch.bfloat16, 3), (kv_pages, "kv_pages", torch.uint8, 3))
     args = (_ptr(k_new, "k_new", torch.bfloat16, (T, Hkv, D), index), _ptr(v_new, "v_new", torch.bfloat16, (T, Hkv, D), index),
             _ptr(slots, "slots", torch.int32, (T,), index), T,
             _ptr(kv_pages, "kv_pages", torch.uint8, (N, Hkv, 17 * D), index))
-    with _device(index):
-        desc = Desc(0, Hkv, Hkv, D, PAGE_SIZE, 1, N, 0, _stream(index), None, 0, *(timing or ()))
-        _check((_lib or load()).sl_kv_write_fp4(ctypes.byref(desc), *args), "sl_kv_write_fp4")
+    if torch._C._cuda_getDevice() != index:
+        with torch.cuda.device(index):
+            return kv_write_fp4(k_new, v_new, slots, kv_pages, timing=timing)
+    desc = Desc(0, Hkv, Hkv, D, PAGE_SIZE, 1, N, 0, _stream(index), None, 0, *(timing or ()))
+    _check((_lib or load()).sl_kv_write_fp4(ctypes.byref(desc), *args), "sl_kv_write_fp4")
 
 
 def kv_read_fp4(slots, kv_pages, *, k_out=None, v_out=None, timing=None) -> tuple[torch.Tensor, torch.Tensor]:
     """``sl_kv_read_fp4``: the key and value rows (bf16 [T, Hkv, D]) in the slots ``slots`` (int32 [T]) of a 4-bit
     cache; zero rows for negative slots, NaN for slots past the pool. Asynchronous on the current stream."""
-    D = _record_dim(kv_pages)
-    N, Hkv, _ = kv_pages.shape
-    T = _shape(slots, "slots", torch.int32, 1)[0]
-    index = kv_pages.get_device()
+    try:
+        (N, Hkv, size), (T,), index = kv_pages.shape, slots.shape, kv_pages.get_device()
+    except _BAD_SIZES:
+        _refuse((kv_pages, "kv_pages", torch.uint8, 3), (slots, "slots", torch.int32, 1))
+    D = size // 17
     pool = _ptr(kv_pages, "kv_pages", torch.uint8, (N, Hkv, 17 * D), index)
     at = _ptr(slots, "slots", torch.int32, (T,), index)
+    if torch._C._cuda_getDevice() != index:
+        with torch.cuda.device(index):
+            return kv_read_fp4(slots, kv_pages, k_out=k_out, v_out=v_out, timing=timing)
     if k_out is None:
         k_out = torch.empty((T, Hkv, D), dtype=torch.bfloat16, device=kv_pages.device)
         k_ptr = k_out.data_ptr()
     else:
         k_ptr = _ptr(k_out, "k_out", torch.bfloat16, (T, Hkv, D), index)
     if v_out is None:
-        v_out = torch.empty((T, Hkv, D), dtype=torch.bfloat16, device=kv_pages.device)
+        v_out = torch.empty_like(k_out)
         v_ptr = v_out.data_ptr()
     else:
         v_ptr = _ptr(v_out, "v_out", torch.bfloat16, (T, Hkv, D), index)
-    with _device(index):
-        desc = Desc(0, Hkv, Hkv, D, PAGE_SIZE, 1, N, 0, _stream(index), None, 0, *(timing or ()))
-        _check((_lib or load()).sl_kv_read_fp4(ctypes.byref(desc), pool, at, T, k_ptr, v_ptr), "sl_kv_read_fp4")
+    desc = Desc(0, Hkv, Hkv, D, PAGE_SIZE, 1, N, 0, _stream(index), None, 0, *(timing or ()))
+    _check((_lib or load()).sl_kv_read_fp4(ctypes.byref(desc), pool, at, T, k_ptr, v_ptr), "sl_kv_read_fp4")
     return k_out, v_out
 
 
@@ -577,14 +584,20 @@ def pages_extend(seq_lens, new_tokens, block_table, free_pages, free_count, max_
     place. Returns ``(seq_lens_out, token_start, slots, free_count_out)``: the new lengths [B], where each request's
     tokens begin in the slot map [B + 1], the slot map [max_tokens] (-1 past the last token), and the pages left.
     ``seq_lens_out`` and ``free_count_out`` may be the inputs themselves. All int32; asynchronous."""
-    B = _shape(seq_lens, "seq_lens", torch.int32, 1)[0]
-    blocks = _shape(block_table, "block_table", torch.int32, 2)[1]
-    N = _shape(free_pages, "free_pages", torch.int32, 1)[0]
-    index = seq_lens.get_device()
+    try:
+        (B,), blocks, (N,), index = seq_lens.shape, block_table.shape[1], free_pages.shape, seq_lens.get_device()
+    except _BAD_SIZES:
+        _refuse((seq_lens, "seq_lens", torch.int32, 1), (block_table, "block_table", torch.int32, 2),
+                (free_pages, "free_pages", torch.int32, 1))
     args = (_ptr(seq_lens, "seq_lens", torch.int32, (B,), index), _ptr(new_tokens, "new_tokens", torch.int32, (B,), index),
             _ptr(block_table, "block_table", torch.int32, (B, blocks), index),
             _ptr(free_pages, "free_pages", torch.int32, (N,), index),
             _ptr(free_count, "free_count", torch.int32, (1,), index), max_tokens)
+    if torch._C._cuda_getDevice() != index:
+        with torch.cuda.device(index):
+            return pages_extend(seq_lens, new_tokens, block_table, free_pages, free_count, max_tokens,
+                                seq_lens_out=seq_lens_out, free_count_out=free_count_out, token_start=token_start,
+                                slots=slots)
     if seq_lens_out is None and free_count_out is None and token_start is None and slots is None:
         # one allocation for all four
         room = torch.empty(2 * B + 2 + max_tokens, dtype=torch.int32, device=seq_lens.device)
@@ -599,30 +612,33 @@ def pages_extend(seq_lens, new_tokens, block_table, free_pages, free_count, max_
                  _ptr(free_count_out, "free_count_out", torch.int32, (1,), index),
                  _ptr(token_start, "token_start", torch.int32, (B + 1,), index),
                  _ptr(slots, "slots", torch.int32, (max_tokens,), index))
-    with _device(index):
-        desc = Desc(B, 1, 1, 64, PAGE_SIZE, blocks, N, 0, _stream(index))
-        _check((_lib or load()).sl_pages_extend(ctypes.byref(desc), *args), "sl_pages_extend")
+    desc = Desc(B, 1, 1, 64, PAGE_SIZE, blocks, N, 0, _stream(index))
+    _check((_lib or load()).sl_pages_extend(ctypes.byref(desc), *args), "sl_pages_extend")
     return seq_lens_out, token_start, slots, free_count_out
 
 
 def pages_release(finished, seq_lens, block_table, free_pages, free_count, *, seq_lens_out=None, free_count_out=None):
     """``sl_pages_release``: the pages of requests with ``finished`` [B] not 0 go back on the stack, in place, and
     their lengths become 0. Returns ``(seq_lens_out, free_count_out)``, which may be the inputs themselves."""
-    B = _shape(seq_lens, "seq_lens", torch.int32, 1)[0]
-    blocks = _shape(block_table, "block_table", torch.int32, 2)[1]
-    N = _shape(free_pages, "free_pages", torch.int32, 1)[0]
-    index = seq_lens.get_device()
+    try:
+        (B,), blocks, (N,), index = seq_lens.shape, block_table.shape[1], free_pages.shape, seq_lens.get_device()
+    except _BAD_SIZES:
+        _refuse((seq_lens, "seq_lens", torch.int32, 1), (block_table, "block_table", torch.int32, 2),
+                (free_pages, "free_pages", torch.int32, 1))
     args = (_ptr(finished, "finished", torch.int32, (B,), index), _ptr(seq_lens, "seq_lens", torch.int32, (B,), index),
             _ptr(block_table, "block_table", torch.int32, (B, blocks), index),
             _ptr(free_pages, "free_pages", torch.int32, (N,), index),
             _ptr(free_count, "free_count", torch.int32, (1,), index))
+    if torch._C._cuda_getDevice() != index:
+        with torch.cuda.device(index):
+            return pages_release(finished, seq_lens, block_table, free_pages, free_count, seq_lens_out=seq_lens_out,
+                                 free_count_out=free_count_out)
     if seq_lens_out is None:
         seq_lens_out = torch.empty_like(seq_lens)
     if free_count_out is None:
         free_count_out = torch.empty_like(free_count)
     args += (_ptr(seq_lens_out, "seq_lens_out", torch.int32, (B,), index),
              _ptr(free_count_out, "free_count_out", torch.int32, (1,), index))
-    with _device(index):
-        desc = Desc(B, 1, 1, 64, PAGE_SIZE, blocks, N, 0, _stream(index))
-        _check((_lib or load()).sl_pages_release(ctypes.byref(desc), *args), "sl_pages_release")
+    desc = Desc(B, 1, 1, 64, PAGE_SIZE, blocks, N, 0, _stream(index))
+    _check((_lib or load()).sl_pages_release(ctypes.byref(desc), *args), "sl_pages_release")
     return seq_lens_out, free_count_out

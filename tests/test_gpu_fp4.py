@@ -158,6 +158,44 @@ def test_attention_sweep(i):
     assert_parity(out, reference(b, pool), f"sweep {i}")
 
 
+@pytest.mark.parametrize("blocks", [1, 2, 127, 128, 129, 300])
+@pytest.mark.parametrize("B,hq,hkv,d", [(3, 28, 4, 128), (70, 32, 8, 64), (7, 32, 2, 64), (300, 16, 1, 128)])
+def test_table_widths(B, hq, hkv, d, blocks):
+    """Tables around the width where short sequences get a workgroup each: lengths of 0, 1, all of the table and others
+    with the default division of the work, and beyond the table and below zero."""
+    _say("table width", B, hq, hkv, d, blocks)
+    rng = np.random.default_rng(blocks)
+    L = np.minimum(rng.integers(0, 16 * blocks + 1, B), np.where(rng.random(B) < 0.3, 16 * blocks, 700))
+    L[0], L[-1] = 16 * blocks, 1
+    L[1] = 0
+    b, pool = make(L, hq, hkv, d, seed=blocks)
+    rows = list(range(min(B, 12)))
+    ref = reference(b, pool, rows)
+    out = sl.decode_attn_fp4(b.q, pool, b.block_table, b.seq_lens, b.scale)
+    torch.cuda.synchronize()
+    assert b.block_table.shape[1] == blocks
+    assert_parity(out[rows], ref, f"{blocks} blocks")
+    lens = b.seq_lens.clone()
+    lens[0], lens[1] = 16 * blocks + 1, -3
+    table = b.block_table.clone()
+    table[2, 0] = pool.shape[0]
+    again = sl.decode_attn_fp4(b.q, pool, table, lens, b.scale)
+    torch.cuda.synchronize()
+    assert torch.isnan(again[:2]).all() and (L[2] == 0 or torch.isnan(again[2]).all())
+    assert torch.equal(again[3:], out[3:])
+
+
+@pytest.mark.parametrize("scale", [-0.3, 0.0, 1e-3, 30.0])
+@pytest.mark.parametrize("workers", [0, 5])
+def test_scales(scale, workers):
+    """Negative, zero, small and large factors; a large one makes the softmax pick single tokens."""
+    b, pool = make([1, 17, 300, 64, 33], 14, 2, 128, seed=12)
+    b.scale = float(np.float32(scale))
+    out = sl.decode_attn_fp4(b.q, pool, b.block_table, b.seq_lens, b.scale, num_workers=workers)
+    torch.cuda.synchronize()
+    assert_parity(out, reference(b, pool), f"scale {scale}")
+
+
 @pytest.mark.parametrize("D", [64, 128])
 def test_one_token_returns_its_value_row(D):
     b, pool = make([1] * 9, 8, 2, D, seed=3)

@@ -76,7 +76,7 @@ def test_the_check_sees_a_branch_over_the_wait():
     assert not early_reads(listing("s_nop 1"))
 
 
-@pytest.mark.parametrize("kernel", ["split_fp4_kernel", "prefix_fp4_kernel"])
+@pytest.mark.parametrize("kernel", ["split_fp4_kernel", "prefix_fp4_kernel", "unit_fp4_kernel"])
 def test_products_are_read_after_their_wait(tmp_path, kernel):
     objdump = os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "llvm", "bin", "llvm-objdump")
     if not os.path.exists(objdump):
