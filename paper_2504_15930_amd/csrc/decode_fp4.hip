@@ -64,8 +64,9 @@ __global__ __launch_bounds__(kWave * kWavesPerBlock) void prefix_fp4_kernel(Spli
         // The four wavefronts of a workgroup are one worker (four column blocks of
         // query rows), or two or four where the largest unit has two blocks or one.
         const int block = (int)blockIdx.x - own_blocks;
-        const int blocks = effective_shared_workers((long long)s_own[B] * own.num_kv_heads, own.num_workers,
-                                                    shared.num_workers, max_shared, NT, kFp4);
+        const int blocks = effective_shared_workers_fp4((long long)s_own[B] * own.num_kv_heads,
+                                                        (long long)s_sh[S] * own.num_kv_heads, per_block,
+                                                        own.num_workers, shared.num_workers, max_shared, NT);
         if (block >= blocks)
             return;
         SplitParams sh = shared;

@@ -249,9 +249,12 @@ __global__ __launch_bounds__(kMergeThreads) void merge_prefix_kernel(PrefixMerge
     const int nw_o = effective_workers(tot_o, p.num_workers, p.step_tiles, wide_from(p.num_workers, p.kv));
     const int nw_s = effective_workers(
         tot_s,
-        shared_workers_of(effective_shared_workers(tot_o, p.num_workers, p.num_shared_workers, p.max_shared_workers,
-                                                   p.step_tiles, p.kv),
-                          per_block, p.num_workers),
+        p.kv == kFp4 ? shared_workers_of(effective_shared_workers_fp4(tot_o, tot_s, per_block, p.num_workers,
+                                                                      p.num_shared_workers, p.max_shared_workers,
+                                                                      p.step_tiles),
+                                         per_block, p.num_workers)
+                     : effective_shared_workers(tot_o, p.num_workers, p.num_shared_workers, p.max_shared_workers,
+                                                p.step_tiles, p.kv),
         p.step_tiles, 0);
     const long long a_o = (long long)Hkv * co + (long long)g * ob;
     const long long a_s = (long long)Hkv * s_start + (long long)g * ss;

@@ -115,6 +115,20 @@ __host__ __device__ inline int effective_shared_workers(long long own_total, int
     const int n = 4 * idle >= 3 * base ? base + (idle < base ? idle : base) : base;
     return n < max_workers ? n : max_workers;
 }
+// The same for an FP4 cache, whose shared pages are bound by instructions: twice
+// `base` also where the shared ranges would be longer than the own ones, as the
+// own-page workgroups then leave their slots before the end. `per_block`: shared
+// workers per workgroup. base -> this rule, MI355X, us:
+//   32 prompts of 4000 tokens x 16 samples (~420 own tokens), 28/4 heads   119 -> 112
+//   130 of 3500 x 14 (~105), 16/1 heads                                    193 -> 166
+// Twice `base` from half as many shared steps on: 64 of 2000 x 4, 64/8 heads 79 and
+// 94 us; 16 of 2000 x 16, 28/4 heads 48 and 59.
+__host__ __device__ inline int effective_shared_workers_fp4(long long own_total, long long shared_total, int per_block,
+                                                            int own_workers, int base, int max_workers, int step_tiles)
+{
+    const int n = effective_shared_workers(own_total, own_workers, base, max_workers, step_tiles, kFp4);
+    return shared_total > own_total * per_block ? (2 * base < max_workers ? 2 * base : max_workers) : n;
+}
 constexpr size_t kAlign = 256;
 
 // ceil(2^32 / group) (2^32 itself, for a group of 1, does not fit): h / group
