@@ -652,7 +652,7 @@ sl_status sl_decode_attn_prefix(const sl_attn_desc *desc, const uint16_t *q, con
                                 float scale, uint16_t *out)
 {
     return sl::run_prefix(desc, q, k_pages, v_pages, nullptr, nullptr, block_table, seq_lens, group_start,
-                          shared_pages, num_groups, scale, out, false);
+                          shared_pages, num_groups, scale, out, sl::kBf16);
 }
 
 sl_status sl_decode_attn_prefix_fp8(const sl_attn_desc *desc, const uint16_t *q, const uint8_t *k_pages,
@@ -661,7 +661,7 @@ sl_status sl_decode_attn_prefix_fp8(const sl_attn_desc *desc, const uint16_t *q,
                                     const int32_t *shared_pages, int32_t num_groups, float scale, uint16_t *out)
 {
     return sl::run_prefix(desc, q, k_pages, v_pages, k_scales, v_scales, block_table, seq_lens, group_start,
-                          shared_pages, num_groups, scale, out, true);
+                          shared_pages, num_groups, scale, out, sl::kE4m3);
 }
 
 sl_status sl_decode_attn_fp4(const sl_attn_desc *desc, const uint16_t *q, const uint8_t *kv_pages,

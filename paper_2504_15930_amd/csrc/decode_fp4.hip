@@ -1,7 +1,9 @@
 // Split-KV decode attention over a 4-bit cache (fp4_unit.h has its layout): the
 // kernels of decode_split.hip and decode_shared.hip for FP4 records.
 //
-// One step is four tiles (17 D bytes each, K and V).
+// Split-KV (split_fp4_kernel), with prefix sharing (prefix_fp4_kernel), and a
+// workgroup per unit for short sequences (unit_fp4_kernel). A step of the split
+// stream is four tiles (17 D bytes each, K and V), elsewhere two.
 #include "prefix_unit.h"
 
 namespace sl {
@@ -145,7 +147,8 @@ __global__ __launch_bounds__(kWave * WAVES) void unit_fp4_kernel(SplitParams p)
             stage_partial<D>(st, l, bad, s_state[wave], G, n, quad);
     }
     __syncthreads();
-    // out = sum of 2^(m_w - M) acc_w / sum of 2^(m_w - M) l_w; a weight of zero drops its state.
+    // out = sum of 2^(m_w - M) acc_w / sum of 2^(m_w - M) l_w. A weight of zero drops its
+    // accumulators, not its sum of weights: a run of nothing but NaN scores has m = -inf, l = NaN.
     for (int i = threadIdx.x; i < G * (D / 4); i += kWave * WAVES) {
         const int row = i / (D / 4), c4 = 4 * (i % (D / 4));
         f32x2_t ml[WAVES];
@@ -160,10 +163,9 @@ __global__ __launch_bounds__(kWave * WAVES) void unit_fp4_kernel(SplitParams p)
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
             const float c = __builtin_amdgcn_exp2f(ml[w][0] - M);
-            if (c != 0.0f) {
+            l += c * ml[w][1];
+            if (c != 0.0f)
                 acc += c * *reinterpret_cast<const f32x4_t *>(s_state[w] + ((size_t)row * D + c4) * 4);
-                l += c * ml[w][1];
-            }
         }
         const float inv = pages == 0 ? (L < 0 ? __builtin_nanf("") : 0.0f) : 1.0f / l;
         if (pages == 0)

@@ -254,7 +254,7 @@ hipError_t launch_extend_pages(const PageParams &p, hipStream_t stream)
     hipError_t e = hipGetLastError();
     if (one || e != hipSuccess)
         return e;
-    hipLaunchKernelGGL(fill_slots_kernel, dim3((p.max_tokens + kSlotTokens - 1) / kSlotTokens), dim3(kSlotThreads),
+    hipLaunchKernelGGL(fill_slots_kernel, dim3(((uint32_t)p.max_tokens + kSlotTokens - 1) / kSlotTokens), dim3(kSlotThreads),
                        sizeof(uint32_t) * ((size_t)p.batch + 1), stream, p);
     return hipGetLastError();
 }

@@ -598,6 +598,8 @@ def pages_extend(seq_lens, new_tokens, block_table, free_pages, free_count, max_
             return pages_extend(seq_lens, new_tokens, block_table, free_pages, free_count, max_tokens,
                                 seq_lens_out=seq_lens_out, free_count_out=free_count_out, token_start=token_start,
                                 slots=slots)
+    if not 0 <= max_tokens < 1 << 31:
+        raise ValueError(f"max_tokens must lie in [0, 2^31), got {max_tokens}")
     if seq_lens_out is None and free_count_out is None and token_start is None and slots is None:
         # one allocation for all four
         room = torch.empty(2 * B + 2 + max_tokens, dtype=torch.int32, device=seq_lens.device)

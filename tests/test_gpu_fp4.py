@@ -271,6 +271,25 @@ def test_nan_and_infinity_reach_their_own_head_only(D, which):
     assert (np.abs(got - ref)[~bad] <= 1e-2 + 2e-2 * np.abs(ref[~bad])).all()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("workers", [0, 7])
+def test_a_nan_key_poisons_from_every_position(D, workers):
+    """Sequence i's key i of one head is NaN, i over all positions: also where it is the only token of a wavefront's
+    share. Its rows are NaN whatever the other shares hold."""
+    n = 147
+    lens = np.maximum(np.arange(n) + 1, np.arange(n) % 5 * 30)
+    b, pool = make(lens, 12, 2, D, seed=61)
+    at = np.arange(n)
+    slots = b.block_table.cpu().numpy()[at, at // 16] * 16 + at % 16
+    k, v = sl.kv_read_fp4(_t(slots), pool)
+    k[:, 1, 3] = float("nan")
+    sl.kv_write_fp4(k, v, _t(slots), pool)
+    out = sl.decode_attn_fp4(b.q, pool, b.block_table, b.seq_lens, b.scale, num_workers=workers)
+    torch.cuda.synchronize()
+    assert torch.isfinite(out[:, :6]).all()
+    assert torch.isnan(out[:, 6:]).all()
+
+
 def test_a_long_pool_past_32_bits():
     """Records beyond the first 4 GB of a pool (and beyond 2^31 bytes) are read and written where they are."""
     D, Hkv = 128, 8
@@ -358,6 +377,27 @@ def test_prefix_odd_groups():
     keep = [i for i in range(24) if i != 7]
     assert torch.isnan(out[7]).all()
     assert_parity(out[keep], ref[keep], "the others")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("workers", [0, 9])
+def test_prefix_a_nan_key_poisons_from_every_position(D, workers):
+    """Key t of one head is NaN: in the first group's prompt it reaches its members' rows of that head, in a member's
+    own tokens that member's alone."""
+    b, starts, shared = inputs.make_grpo_batch(2, 3, 48, seed=8, device=DEV, num_q_heads=12, num_kv_heads=2, head_dim=D,
+                                               gen_median=20, gen_cap=40)
+    pool = quantised(b)
+    for t in range(int(b.seq_lens[1])):
+        slot = _t([int(b.block_table[1, t // 16]) * 16 + t % 16])
+        k, v = sl.kv_read_fp4(slot, pool)
+        k2 = k.clone()
+        k2[:, 1, 3] = float("nan")
+        sl.kv_write_fp4(k2, v, slot, pool)
+        out = sl.decode_attn_prefix_fp4(b.q, pool, b.block_table, b.seq_lens, b.scale, starts, shared, num_workers=workers)
+        bad = torch.zeros(out.shape[:2], dtype=torch.bool, device=DEV)
+        bad[slice(0, 3) if t < 48 else slice(1, 2), 6:] = True
+        assert torch.isnan(out[bad]).all() and torch.isfinite(out[~bad]).all(), t
+        sl.kv_write_fp4(k, v, slot, pool)     # (stored values come back as they were)
 
 
 def test_prefix_largest_batch():

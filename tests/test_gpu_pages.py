@@ -76,6 +76,25 @@ def test_extend_many_tokens():
             _check_extend(lens, new, table, free, B * blocks, c)
 
 
+def test_extend_largest_slot_map():
+    """2^31 - 1 entries, the most that the argument holds, of which three are tokens."""
+    tl, tt, tf, tc = _t([14]), _t([[5, -9]]), _t([0, 1, 2, 4, 3, -3]), _t([5])
+    cap = 2**31 - 1
+    slots = torch.full((cap,), 7, dtype=torch.int32, device=DEV)
+    sl.pages_extend(tl, _t([3]), tt, tf, tc, cap, slots=slots)
+    torch.cuda.synchronize()
+    assert slots[:3].tolist() == [5 * 16 + 14, 5 * 16 + 15, 3 * 16]
+    assert (slots[3:] == -1).all() and tt.tolist() == [[5, 3]]
+
+
+@pytest.mark.parametrize("cap", [-1, 2**31, 2**32 + 8])
+def test_extend_slot_map_size_refusals(cap):
+    tl, tt, tf, tc = _t([14]), _t([[5, -9]]), _t([0, 1, 2, 4, 3, -3]), _t([5])
+    for kw in ({}, dict(slots=_t(np.zeros(8)))):
+        with pytest.raises(ValueError):
+            sl.pages_extend(tl, _t([3]), tt, tf, tc, cap, **kw)
+
+
 def test_extend_without_room():
     """A short stack and a short slot map: requests are served in order while there is room, those that need none too."""
     rng = np.random.default_rng(2)
