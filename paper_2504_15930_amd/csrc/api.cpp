@@ -187,6 +187,24 @@ int unit_waves(const sl_attn_desc *d, int kv)
     return (long long)d->batch * d->num_kv_heads <= 256 ? 8 : 4;
 }
 
+// The same for prefix sharing. Reading the shared pages once costs the products of
+// 16-row blocks, the scans and a merge; attending every member by itself costs its
+// tiles again, out of the caches. Prefix kernel -> a workgroup per unit:
+//   prompts x samples of prompt, heads, D        units x blocks
+//   3 x 22 of 1000, 12/12, 64                         53064   20.0 -> 14.6
+//   8 x 8 of 500, 28/4, 128                           14592   21.2 ->  8.8
+//   16 x 16 of 1000, 28/4, 128                       121856   34.7 -> 23.2
+//   64 x 16 of 800, 28/4, 128                        258048   77.3 -> 57.7
+//   64 x 16 of 1800, 28/4, 128                       512000  105.7 -> 112.4
+//   128 x 4 of 500, 32/8, 64                         180224   40.6 -> 30.8
+//   16 x 16 of 1800, 32/8, 64                        256000   34.7 -> 39.5
+int unit_waves_prefix(const sl_attn_desc *d, int kv, int num_groups)
+{
+    const long long most = d->head_dim == 128 ? 400000 : 200000;
+    const bool few = (long long)d->batch * d->num_kv_heads * d->max_blocks_per_seq <= most;
+    return few && num_groups <= kUnitGroups ? unit_waves(d, kv) : 0;
+}
+
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
@@ -248,7 +266,7 @@ sl_status run(const sl_attn_desc *d, const uint16_t *q, const void *k_pages, con
     if (d->timing_start && hipEventRecord(d->timing_start, d->stream) != hipSuccess)
         return SL_ERR_HIP;
     if (const int waves = unit_waves(d, kv)) {
-        if (launch_unit_fp4(sp, waves, d->head_dim, d->stream) != hipSuccess ||
+        if (launch_unit_fp4(sp, UnitGroups{nullptr, nullptr, 0}, waves, d->head_dim, d->stream) != hipSuccess ||
             (d->timing_stop && hipEventRecord(d->timing_stop, d->stream) != hipSuccess))
             return SL_ERR_HIP;
         return SL_OK;
@@ -415,6 +433,13 @@ sl_status run_prefix(const sl_attn_desc *d, const uint16_t *q, const void *k_pag
     sp_.unit_acc = ws.own_unit_acc;
     if (d->timing_start && hipEventRecord(d->timing_start, d->stream) != hipSuccess)
         return SL_ERR_HIP;
+    if (const int waves = unit_waves_prefix(d, kv, num_groups)) {
+        if (launch_unit_fp4(sp_, UnitGroups{group_start, shared_pages, num_groups}, waves, d->head_dim, d->stream) !=
+                hipSuccess ||
+            (d->timing_stop && hipEventRecord(d->timing_stop, d->stream) != hipSuccess))
+            return SL_ERR_HIP;
+        return SL_OK;
+    }
     if (launch_prefix_split(sp_, shp, nws_max, pp, d->head_dim, kv, d->stream) != hipSuccess)
         return SL_ERR_HIP;
     if (d->timing_stop && hipEventRecord(d->timing_stop, d->stream) != hipSuccess)

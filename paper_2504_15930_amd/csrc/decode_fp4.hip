@@ -79,7 +79,24 @@ __global__ __launch_bounds__(kWave * kWavesPerBlock) void prefix_fp4_kernel(Spli
     }
 }
 
-// Plain attention where every sequence is short (a block table of at most
+// Whether this thread's group holds sequence b and shares more pages than its L
+// tokens fill: shared as scan_prefix_groups has it, in range and at or after the
+// end of every earlier group's range.
+__device__ __forceinline__ bool cut_short(const UnitGroups &g, const SplitParams &p, int b, int L)
+{
+    const int k = threadIdx.x;
+    if (k >= g.count)
+        return false;
+    const int lo = g.start[k], hi = g.start[k + 1], sp = g.shared_pages[k];
+    if (lo < 0 || b < lo || b >= hi || hi > p.batch || sp <= 0 || sp > p.max_blocks || L >= sp * kPageSize)
+        return false;
+    for (int j = 0; j < k; ++j)   // (only on the way to a NaN row)
+        if (g.start[j + 1] > lo)
+            return false;
+    return true;
+}
+
+// Attention where every sequence is short (a block table of at most
 // kUnitBlocks entries): one workgroup per unit, its tiles dealt to the wavefronts
 // in contiguous runs of whole steps, their states combined in LDS. One launch, no
 // scan of the batch, no partial states in memory, two trips to memory before the
@@ -87,8 +104,12 @@ __global__ __launch_bounds__(kWave * kWavesPerBlock) void prefix_fp4_kernel(Spli
 // that latency, and with thousands of units by instructions, as the stream is.
 // Steps of two tiles: with four, fewer workgroups fit a CU (384 x 1..1024, 32/8
 // heads, D = 64 29.6 us instead of 26.4; 512 x 1..256, 64/8 heads 40.5 and 26.0).
+// With prefix sharing the members' rows of a prompt are attended one by one too
+// (its pages come out of the caches): the groups only decide which member is
+// shorter than its group's shared pages. A thread looks at one group, in the
+// first trip to memory.
 template <int D, int KV, int WAVES>
-__global__ __launch_bounds__(kWave * WAVES) void unit_fp4_kernel(SplitParams p)
+__global__ __launch_bounds__(kWave * WAVES) void unit_fp4_kernel(SplitParams p, UnitGroups groups)
 {
     constexpr int NT = kUnitStepTiles;
     constexpr bool HALF = KV == kFp4Half;
@@ -107,7 +128,8 @@ __global__ __launch_bounds__(kWave * WAVES) void unit_fp4_kernel(SplitParams p)
     // Lane i: the address of tile i of the run (those past it: the last one's).
     const int page = p.block_table[(size_t)b * p.max_blocks + max(0, min(first * NT + min(lane, tiles - 1), pages - 1))];
     const bool in = page >= 0 && page < p.num_pages;
-    const bool bad = L < 0 || L > max_len || __builtin_amdgcn_ballot_w64(lane < tiles && !in) != 0;
+    const bool mine = cut_short(groups, p, b, L) || (lane < tiles && !in);
+    const bool bad = L < 0 || L > max_len || __builtin_amdgcn_ballot_w64(mine) != 0;
     const uint64_t record = reinterpret_cast<uint64_t>(p.k_pages) +
                             (in ? (uint64_t)(uint32_t)(page * Hkv + g) * (uint32_t)fp4_record_bytes(D) : 0u);
     u32x4_t q[D / 32];
@@ -167,9 +189,14 @@ __global__ __launch_bounds__(kWave * WAVES) void unit_fp4_kernel(SplitParams p)
             if (c != 0.0f)
                 acc += c * *reinterpret_cast<const f32x4_t *>(s_state[w] + ((size_t)row * D + c4) * 4);
         }
-        const float inv = pages == 0 ? (L < 0 ? __builtin_nanf("") : 0.0f) : 1.0f / l;
-        if (pages == 0)
+        float inv = 1.0f / l;
+        if (pages == 0) {   // zero, or NaN where a wavefront found the sequence invalid
             acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            inv = 0.0f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w)
+                inv = ml[w][0] != ml[w][0] ? ml[w][0] : inv;
+        }
         *reinterpret_cast<u32x2_t *>(p.out + ((size_t)unit * G + row) * D + c4) =
             u32x2_t{pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv)};
     }
@@ -179,7 +206,7 @@ __global__ __launch_bounds__(kWave * WAVES) void unit_fp4_kernel(SplitParams p)
 
 namespace {
 template <int WAVES>
-SplitKernel unit_kernel(int head_dim, int group)
+UnitKernel unit_kernel(int head_dim, int group)
 {
     if (head_dim == 128)
         return group <= 8 ? unit_fp4_kernel<128, kFp4Half, WAVES> : unit_fp4_kernel<128, kFp4, WAVES>;
@@ -189,12 +216,13 @@ SplitKernel unit_kernel(int head_dim, int group)
 }
 }  // namespace
 
-hipError_t launch_unit_fp4(const SplitParams &p, int waves, int head_dim, hipStream_t stream)
+hipError_t launch_unit_fp4(const SplitParams &p, const UnitGroups &groups, int waves, int head_dim,
+                           hipStream_t stream)
 {
-    const SplitKernel kernel = waves == 8 ? unit_kernel<8>(head_dim, p.group) : unit_kernel<4>(head_dim, p.group);
+    const UnitKernel kernel = waves == 8 ? unit_kernel<8>(head_dim, p.group) : unit_kernel<4>(head_dim, p.group);
     if (!kernel)
         return hipErrorInvalidValue;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.batch * p.num_kv_heads)), dim3(kWave * waves), 0, stream, p);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.batch * p.num_kv_heads)), dim3(kWave * waves), 0, stream, p, groups);
     return hipGetLastError();
 }
 

@@ -315,14 +315,23 @@ inline size_t prefix_dynamic_lds(int batch, int max_sub)
 {
     return sizeof(int32_t) * (3 * (size_t)batch + 2 * (size_t)max_sub + 3);
 }
-// Plain attention over a 4-bit cache with one workgroup per unit: tables of at
-// most this many blocks (at most 256, as each of four wavefronts keeps its run's
-// addresses in its lanes), and tiles per step.
+// Attention over a 4-bit cache with one workgroup per unit: tables of at most
+// this many blocks (at most 256, as each of four wavefronts keeps its run's
+// addresses in its lanes), tiles per step, and groups with shared pages (a
+// thread of the smaller workgroup each).
 constexpr int kUnitBlocks = 128;
 constexpr int kUnitStepTiles = 2;
+constexpr int kUnitGroups = 4 * kWave;
+struct UnitGroups {
+    const int32_t *start;          // [count + 1]
+    const int32_t *shared_pages;   // [count]
+    int32_t count;                 // 0: no prefix sharing
+};
 using SplitKernel = void (*)(SplitParams);
+using UnitKernel = void (*)(SplitParams, UnitGroups);
 using PrefixKernel = void (*)(SplitParams, SplitParams, PrefixParams, int, int);
-hipError_t launch_unit_fp4(const SplitParams &p, int waves, int head_dim, hipStream_t stream);   // decode_fp4.hip
+hipError_t launch_unit_fp4(const SplitParams &p, const UnitGroups &groups, int waves, int head_dim,
+                           hipStream_t stream);               // decode_fp4.hip
 SplitKernel split_fp4_kernel_of(int head_dim, int group);     // decode_fp4.hip (null: no such head_dim)
 PrefixKernel prefix_fp4_kernel_of(int head_dim, int group);
 hipError_t launch_split(const SplitParams &p, int head_dim, int kv, hipStream_t stream);

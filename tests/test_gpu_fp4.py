@@ -379,6 +379,33 @@ def test_prefix_odd_groups():
     assert_parity(out[keep], ref[keep], "the others")
 
 
+@pytest.mark.parametrize("case", [(3, 5, 2100, 28, 4, 128, 30, 200), (2, 9, 2070, 16, 4, 64, 20, 100),
+                                  (3, 3, 2050, 12, 12, 64, 30, 90), (300, 2, 40, 8, 2, 128, 10, 30)])
+def test_prefix_past_the_short_tables(case):
+    """More than 128 blocks per sequence, or more than 256 groups."""
+    test_prefix_shapes(case, 0)
+
+
+@pytest.mark.parametrize("workers", [0, 5])
+def test_prefix_short_members(workers):
+    """A member shorter than its prompt's shared pages gets NaN rows; in a range that is not shared (it starts before an
+    earlier one's end) the same length is attended as it is."""
+    b, starts, shared = inputs.make_grpo_batch(4, 6, 100, seed=3, device=DEV, num_q_heads=8, num_kv_heads=2, head_dim=64,
+                                               gen_median=40, gen_cap=90)
+    pool = quantised(b)
+    for i in (2, 7, 15):
+        b.seq_lens[i] = 95
+    b.seq_lens[20] = 0
+    ref = reference(b, pool)
+    for gs, sp, short in ((starts, shared, [2, 7, 15, 20]), (_t([6, 12, 0, 6, 24]), shared, [7]),
+                          (_t([0, 6, 12, 30, 24]), shared, [2, 7]), (starts, torch.zeros_like(shared), [])):
+        out = sl.decode_attn_prefix_fp4(b.q, pool, b.block_table, b.seq_lens, b.scale, gs, sp, num_workers=workers)
+        torch.cuda.synchronize()
+        keep = [i for i in range(24) if i not in short]
+        assert torch.isnan(out[short]).all()
+        assert_parity(out[keep], ref[keep], f"groups {gs.tolist()} {sp.tolist()}")
+
+
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("workers", [0, 9])
 def test_prefix_a_nan_key_poisons_from_every_position(D, workers):
