@@ -157,6 +157,7 @@ __global__ __launch_bounds__(kWave * WAVES) void unit_fp4_kernel(SplitParams p, 
         for (int k = 0; k < 2; ++k) {
             const int i = i0 + k;
             issue(buf[1 - k], i + 1);
+            __builtin_amdgcn_sched_barrier(0);   // (else the first products wait for their tiles before these loads)
             if (i < count)
                 fp4_step<D, NT>(state, buf[k], qop, mul, min(kPageSize * NT, L - kPageSize * NT * (first + i)), n,
                                 quad);

@@ -145,6 +145,17 @@ __device__ __forceinline__ void fp4_step(Fp4State<D, HALF> &st, const T (&t)[N],
     static_assert(HALF || NT == 1 || NT % 2 == 0, "one tile, or pairs of tiles, per step");
     const bool partial = valid < kPageSize * NT;
     auto dead = [&](int u, int r) { return kPageSize * u + 4 * quad + r >= valid; };
+    // In a step of four tiles the compiler makes two copies of the code by itself; in
+    // a smaller one it keeps the masks under branches, and their comparisons, if it
+    // can, before them, in every step. There every branch has its own `valid`. (Two
+    // copies written out took 170 registers for 110 in unit_fp4_kernel of D = 128:
+    // 512 x 1..256 tokens, 64/8 heads, 26 -> 35 us.)
+    constexpr bool kBranches = NT < 4;
+    auto own = [&](int v) {
+        if (kBranches)
+            asm volatile("" : "+s"(v));
+        return v;
+    };
     f32x4_t s4[NT];
 #pragma unroll
     for (int u = 0; u < NT; ++u)
@@ -171,11 +182,12 @@ __device__ __forceinline__ void fp4_step(Fp4State<D, HALF> &st, const T (&t)[N],
     };
     auto mask = [&](auto &y) {
         if (partial) {
+            const int live = own(valid) - 4 * quad;
 #pragma unroll
             for (int u = 0; u < NT; ++u)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    y[u][r] = dead(u, r) ? kNegInf : y[u][r];
+                    y[u][r] = kPageSize * u + r >= live ? kNegInf : y[u][r];
         }
     };
     auto largest = [&](const auto &y) {
@@ -185,9 +197,22 @@ __device__ __forceinline__ void fp4_step(Fp4State<D, HALF> &st, const T (&t)[N],
             top = fmaxf(top, fmaxf(fmaxf(y[u][0], y[u][1]), fmaxf(y[u][2], y[u][3])));
         return top;
     };
+    // (An instruction written out: out of a branch the compiler first makes every value canonical.)
+    auto largest_of = [&](const float(&y)[NT][4]) {
+        auto max3 = [](float a, float b, float c) {
+            float top;
+            asm("v_max3_f32 %0, %1, %2, %3" : "=v"(top) : "v"(a), "v"(b), "v"(c));
+            return top;
+        };
+        float top = y[0][0];
+#pragma unroll
+        for (int i = 1; i < 4 * NT; i += 2)
+            top = max3(top, y[i / 4][i % 4], i + 1 < 4 * NT ? y[(i + 1) / 4][(i + 1) % 4] : y[i / 4][i % 4]);
+        return top;
+    };
     exponents();
     mask(x);
-    if (__builtin_amdgcn_ballot_w64(largest(x) > kRescaleSlack) != 0) {
+    if (__builtin_amdgcn_ballot_w64(largest_of(x) > kRescaleSlack) != 0) {
         mask(s4);
         const float mx = quad_max(largest(s4) * mul);
         if (mx > st.m + kRescaleSlack) {
@@ -207,13 +232,29 @@ __device__ __forceinline__ void fp4_step(Fp4State<D, HALF> &st, const T (&t)[N],
 #pragma unroll
         for (int r = 0; r < 4; ++r)
             p[u][r] = __builtin_amdgcn_exp2f(x[u][r]);
-    // A dead token's codes are finite, its scale need not be.
+    // A dead token's codes are finite, its scale need not be: 1 in its place, by a
+    // selection, or a byte put into the scales before.
+    uint32_t vs[NT];
+    if (kBranches) {
+#pragma unroll
+        for (int u = 0; u < NT; ++u)
+            vs[u] = t[u].vs;
+        if (partial) {
+            const int live = own(valid) - 4 * quad;
+#pragma unroll
+            for (int u = 0; u < NT; ++u)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    vs[u] = kPageSize * u + r >= live ? (vs[u] & ~(0xffu << 8 * r)) | 127u << 8 * r : vs[u];
+        }
+    }
     auto v_scale = [&](int u, int r) {
-        const float s = r == 0   ? e8m0_byte<0>(t[u].vs)
-                        : r == 1 ? e8m0_byte<1>(t[u].vs)
-                        : r == 2 ? e8m0_byte<2>(t[u].vs)
-                                 : e8m0_byte<3>(t[u].vs);
-        return partial && dead(u, r) ? 1.0f : s;
+        const uint32_t from = kBranches ? vs[u] : t[u].vs;
+        const float s = r == 0   ? e8m0_byte<0>(from)
+                        : r == 1 ? e8m0_byte<1>(from)
+                        : r == 2 ? e8m0_byte<2>(from)
+                                 : e8m0_byte<3>(from);
+        return !kBranches && partial && dead(u, r) ? 1.0f : s;
     };
     constexpr uint32_t kOnes = 0x3f803f80u;
     const bf16x8_t ones = __builtin_bit_cast(bf16x8_t, u32x4_t{kOnes, kOnes, kOnes, kOnes});
