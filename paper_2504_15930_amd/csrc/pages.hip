@@ -7,7 +7,12 @@
 // workgroup holds the batch (at most kMaxBatch requests, eight per thread) and
 // forms them with two scans, so the lengths and the count may be updated in
 // place; it finds a page's or a token's request by binary search in the sums,
-// which it keeps in LDS. Bound by latency: a few dependent trips to memory.
+// which it keeps in LDS. Many pages and a long slot map are shared among
+// workgroups that all form the sums for themselves, if nothing that they read is
+// updated in place; else one workgroup moves the pages, and a second launch makes
+// the slot map. Bound by latency: a few dependent trips to memory.
+#include <algorithm>
+
 #include "sl_internal.h"
 #include "wave_ops.h"
 
@@ -83,13 +88,16 @@ __device__ __forceinline__ uint32_t stack_size(const PageParams &p)
     return (uint32_t)max(0, min(n, p.num_pages));
 }
 
-// `with_slots`: the slot map too; else fill_slots_kernel follows.
+// `slots_per_block`: entries of the slot map that each workgroup makes; none if
+// 0, and fill_slots_kernel follows. With several workgroups, those enter the opened
+// pages in turn, and the first one writes the rest.
 template <int PER>
-__global__ __launch_bounds__(kPageThreads) void extend_pages_kernel(PageParams p, int with_slots)
+__global__ __launch_bounds__(kPageThreads) void extend_pages_kernel(PageParams p, uint32_t slots_per_block)
 {
     extern __shared__ uint32_t s_dyn[];
     __shared__ uint32_t s_wave[kPageWaves][2];
     const int B = p.batch, tid = threadIdx.x;
+    const bool one = blockIdx.x == 0;
     uint32_t *const s_tok = s_dyn;            // [B + 1] tokens of the requests before
     uint32_t *const s_pg = s_tok + B + 1;     // [B + 1] pages that they open
     uint32_t *const s_len = s_pg + B + 1;     // [B] lengths so far
@@ -133,8 +141,10 @@ __global__ __launch_bounds__(kPageThreads) void extend_pages_kernel(PageParams p
             s_tok[b] = got_tok;
             s_pg[b] = got_pg;
             s_len[b] = (uint32_t)len[i];
-            p.token_start[b] = (int32_t)got_tok;
-            p.seq_lens_out[b] = len[i] + (int32_t)add[i];
+            if (one) {
+                p.token_start[b] = (int32_t)got_tok;
+                p.seq_lens_out[b] = len[i] + (int32_t)add[i];
+            }
         }
         got_tok += add[i];
         got_pg += open[i];
@@ -142,17 +152,18 @@ __global__ __launch_bounds__(kPageThreads) void extend_pages_kernel(PageParams p
     if (tid == 0) {
         s_tok[B] = all_tok;
         s_pg[B] = all_pg;
-        p.token_start[B] = (int32_t)all_tok;
-        p.free_count_out[0] = (int32_t)(count - all_pg);
+        if (one) {
+            p.token_start[B] = (int32_t)all_tok;
+            p.free_count_out[0] = (int32_t)(count - all_pg);
+        }
     }
     __syncthreads();
-    for (uint32_t x = tid; x < all_pg; x += kPageThreads) {
+    for (uint32_t x = blockIdx.x * kPageThreads + tid; x < all_pg; x += gridDim.x * kPageThreads) {
         const int b = find(s_pg, B, x);
         p.block_table[(size_t)b * p.max_blocks + blocks_of((int)s_len[b]) + (x - s_pg[b])] = p.free_pages[count - 1 - x];
     }
-    if (!with_slots)
-        return;
-    for (uint32_t x = tid; x < (uint32_t)p.max_tokens; x += kPageThreads) {
+    const uint32_t from = blockIdx.x * slots_per_block, to = min(from + slots_per_block, (uint32_t)p.max_tokens);
+    for (uint32_t x = from + tid; x < to; x += kPageThreads) {
         int32_t slot = -1;
         if (x < all_tok) {
             const int b = find(s_tok, B, x);
@@ -223,46 +234,63 @@ __global__ __launch_bounds__(kPageThreads) void release_pages_kernel(PageParams 
         const int b = first + i;
         if (i < per && b < B) {
             s_pg[b] = pg;
-            p.seq_lens_out[b] = len[i];
+            if (blockIdx.x == 0)
+                p.seq_lens_out[b] = len[i];
         }
         pg += back[i];
     }
     const uint32_t room = (uint32_t)p.num_pages - count;   // (pages given back twice do not fit)
     if (tid == 0) {
         s_pg[B] = all;
-        p.free_count_out[0] = (int32_t)(count + min(all, room));
+        if (blockIdx.x == 0)
+            p.free_count_out[0] = (int32_t)(count + min(all, room));
     }
     __syncthreads();
-    for (uint32_t x = tid; x < min(all, room); x += kPageThreads) {   // a request's last block first
+    // (a request's last block first)
+    for (uint32_t x = blockIdx.x * kPageThreads + tid; x < min(all, room); x += gridDim.x * kPageThreads) {
         const int b = find(s_pg, B, x);
         p.free_pages[count + x] = p.block_table[(size_t)b * p.max_blocks + (s_pg[b + 1] - 1 - x)];
     }
 }
 
-// Tokens up to which the first launch makes the slot map as well.
-constexpr int kOneLaunchTokens = 4096;
+// Entries of the slot map, or of the block table, per workgroup, at least: below
+// four per thread the scans, which every workgroup repeats, would be most of its
+// work. Workgroups at most, one per CU.
+constexpr uint32_t kItemsPerBlock = 4 * kPageThreads;
+constexpr uint32_t kMostBlocks = 256;
+
+// Neither the lengths nor the count is updated in place.
+bool apart(const PageParams &p) { return p.seq_lens_out != p.seq_lens && p.free_count_out != p.free_count; }
 
 }  // namespace
 
 // (One request per thread where that is enough: the code for eight is four times
 // as long, and a first pass through it is instruction fetches.)
+// Call with 1024 requests of 1000 tokens: 11.8 us, with one workgroup for the
+// pages and a second launch 65; 96 of 1365: 11.8 and 14.6; 8192 of 100: 24 and 92.
 hipError_t launch_extend_pages(const PageParams &p, hipStream_t stream)
 {
-    const bool one = p.max_tokens <= kOneLaunchTokens;
-    hipLaunchKernelGGL(p.batch <= kPageThreads ? extend_pages_kernel<1> : extend_pages_kernel<kMostPer>, dim3(1),
-                       dim3(kPageThreads), sizeof(uint32_t) * (3 * (size_t)p.batch + 2), stream, p, one ? 1 : 0);
+    const uint32_t tokens = (uint32_t)p.max_tokens;
+    const uint32_t each = std::max(kItemsPerBlock, (tokens + kMostBlocks - 1) / kMostBlocks);
+    const bool one_launch = apart(p) || tokens <= kItemsPerBlock;
+    const uint32_t blocks = one_launch && tokens > 0 ? (tokens + each - 1) / each : 1;
+    hipLaunchKernelGGL(p.batch <= kPageThreads ? extend_pages_kernel<1> : extend_pages_kernel<kMostPer>, dim3(blocks),
+                       dim3(kPageThreads), sizeof(uint32_t) * (3 * (size_t)p.batch + 2), stream, p,
+                       one_launch ? each : 0u);
     hipError_t e = hipGetLastError();
-    if (one || e != hipSuccess)
+    if (one_launch || e != hipSuccess)
         return e;
-    hipLaunchKernelGGL(fill_slots_kernel, dim3(((uint32_t)p.max_tokens + kSlotTokens - 1) / kSlotTokens), dim3(kSlotThreads),
+    hipLaunchKernelGGL(fill_slots_kernel, dim3((tokens + kSlotTokens - 1) / kSlotTokens), dim3(kSlotThreads),
                        sizeof(uint32_t) * ((size_t)p.batch + 1), stream, p);
     return hipGetLastError();
 }
 
 hipError_t launch_release_pages(const PageParams &p, hipStream_t stream)
 {
-    hipLaunchKernelGGL(p.batch <= kPageThreads ? release_pages_kernel<1> : release_pages_kernel<kMostPer>, dim3(1),
-                       dim3(kPageThreads), sizeof(uint32_t) * ((size_t)p.batch + 1), stream, p);
+    const uint64_t pages = (uint64_t)p.batch * (uint64_t)p.max_blocks;   // at most
+    const uint64_t blocks = apart(p) ? std::min<uint64_t>(kMostBlocks, pages / kItemsPerBlock + 1) : 1;
+    hipLaunchKernelGGL(p.batch <= kPageThreads ? release_pages_kernel<1> : release_pages_kernel<kMostPer>,
+                       dim3((unsigned)blocks), dim3(kPageThreads), sizeof(uint32_t) * ((size_t)p.batch + 1), stream, p);
     return hipGetLastError();
 }
 

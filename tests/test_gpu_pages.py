@@ -63,8 +63,9 @@ def test_extend(B, blocks, in_place):
         _check_extend(lens, new, table, free, B * blocks, int(new.sum()) + 3, in_place)
 
 
-def test_extend_many_tokens():
-    """Slot maps of more tokens than one launch fills."""
+@pytest.mark.parametrize("in_place", [False, True])
+def test_extend_many_tokens(in_place):
+    """Slot maps of more tokens than one workgroup fills."""
     rng = np.random.default_rng(1)
     for B, blocks in ((1, 2000), (5, 1200), (300, 60)):
         print("many tokens", B, blocks, flush=True)
@@ -73,7 +74,21 @@ def test_extend_many_tokens():
         new[0] = blocks * 16 - lens[0]
         cap = int(new.sum())
         for c in (cap, cap + 1, max(cap - 1, 0), cap + 5000):
-            _check_extend(lens, new, table, free, B * blocks, c)
+            _check_extend(lens, new, table, free, B * blocks, c, in_place)
+
+
+def test_extend_one_output_in_place():
+    """The lengths or the count alone updated in place, with a slot map of more tokens than one workgroup fills."""
+    lens, table, free = _case(np.random.default_rng(8), 40, 60, 2400)
+    new = 60 * 16 - lens
+    cap = int(new.sum())
+    want = fp4.pages_extend(lens, new, table, free, 2400, cap)
+    for name in ("seq_lens_out", "free_count_out"):
+        tl, tt, tf, tc = _t(lens), _t(table), _t(free), _t([2400])
+        got = sl.pages_extend(tl, _t(new), tt, tf, tc, cap, **{name: tl if name == "seq_lens_out" else tc})
+        torch.cuda.synchronize()
+        assert [x.tolist() for x in got[:3]] == [list(x) for x in want[:3]] and got[3].item() == want[3], name
+        assert np.array_equal(tt.cpu().numpy(), want[4])
 
 
 def test_extend_largest_slot_map():
@@ -123,7 +138,7 @@ def test_extend_invalid_data():
 
 
 @pytest.mark.parametrize("in_place", [False, True])
-@pytest.mark.parametrize("B,blocks", [(1, 1), (7, 3), (64, 9), (256, 40), (1025, 3), (8192, 2)])
+@pytest.mark.parametrize("B,blocks", [(1, 1), (7, 3), (64, 9), (256, 40), (1025, 3), (8192, 2), (96, 300), (2000, 40)])
 def test_release(B, blocks, in_place):
     print("release", B, blocks, flush=True)
     rng = np.random.default_rng(B + blocks)
