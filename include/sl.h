@@ -287,7 +287,8 @@ sl_status sl_kv_append_fp8(const sl_attn_desc *desc, const uint16_t *k_new, cons
  * -126 <= e <= 125; every element is the nearest code of x / 2^e, ties to even,
  * saturating at 6 (only from a >= 7 2^125 on). So |stored - x| <= max(|x| / 4,
  * 2^e / 4), and exact for zeros. A block with a NaN or an infinity is stored as
- * s = 255 with zero codes. A token owns whole bytes of a record: writing one row
+ * s = 255 with zero codes (so s is 1 .. 252 or 255 in what is written here; every
+ * byte is read as above). A token owns whole bytes of a record: writing one row
  * neither reads nor changes its neighbours.
  *
  * Decode attention over a 4-bit cache; the cached values are as above, and

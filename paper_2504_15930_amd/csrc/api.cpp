@@ -143,9 +143,9 @@ sl_status resolve_workers(const sl_attn_desc *d, int kv, int *nw, bool prefix = 
     // were slower for all but E4M3 with head_dim 64 and one tile per step.
     // A 4-bit cache with head_dim 64 takes two per CU: its tiles are so short that
     // instructions set the pace, and one wavefront's fill the other's waits (384
-    // sequences of 1..2048 tokens, 32/8 heads: 51.6 us, with one 59.4). With head_dim
-    // 128 two were slower (512 x 512 + lognormal(2048), 28/4 heads: 173 us with one,
-    // 188 with two; 256 of 64/8 heads 350 and 368).
+    // sequences of 1..2048 tokens, 32/8 heads: 52.4 us, with one 60.7). With head_dim
+    // 128 two were slower (512 x 512 + lognormal(2048), 28/4 heads: 174 us with one,
+    // 187 with two; 256 of 64/8 heads 350 and 367).
     // Prefix-shared attention keeps one own-page workgroup per CU beside its shared-page
     // workgroups (three per four CUs was 12% slower).
     const int blocks = info->blocks[d->head_dim == 128][kv];
@@ -173,12 +173,12 @@ int shared_workers(int nw) { return nw / 4 > 0 ? nw / 4 : 1; }
 // workgroup a CU. Calls, split and merge -> a workgroup per unit, MI355X, tokens
 // 1 .. 16 times the table's blocks:
 //   blocks                 16             64            128               256
-//   5 x 28/4 heads                   13.0 ->  9.5   13.0 ->  9.7
-//   64 x 28/4          13.2 ->  9.5  15.3 ->  9.4   17.3 -> 12.0   22.0 -> 19.0
-//   256 x 28/4                       20.6 -> 12.1   34.2 -> 29.4   56.3 -> 58.7
-//   512 x 64/8         37.1 -> 26.0  71.4 -> 57.2
-//   384 x 32/8, D = 64 19.6 -> 13.6  35.6 -> 26.4   52.3 -> 44.9   90.5 -> 87.0
-//   4 x 32/8, D = 64                                               13.0 -> 14.5
+//   5 x 28/4 heads                   13.0 ->  8.0   12.4 ->  9.3
+//   64 x 28/4          13.1 ->  8.8  14.9 ->  8.6   17.3 -> 11.5   22.0 -> 19.0
+//   256 x 28/4                       26.5 -> 16.1   35.2 -> 27.6   57.4 -> 58.7
+//   512 x 64/8         36.4 -> 25.3  73.3 -> 56.7
+//   384 x 32/8, D = 64 20.1 -> 12.9  35.8 -> 25.5   53.2 -> 44.4   92.0 -> 87.0
+//   4 x 32/8, D = 64                                               12.9 -> 14.5
 // (512 x 64/8 of 16 blocks with eight wavefronts 42.6, 64 x 28/4 of 128 with four 13.4.)
 int unit_waves(const sl_attn_desc *d, int kv)
 {
@@ -191,13 +191,15 @@ int unit_waves(const sl_attn_desc *d, int kv)
 // 16-row blocks, the scans and a merge; attending every member by itself costs its
 // tiles again, out of the caches. Prefix kernel -> a workgroup per unit:
 //   prompts x samples of prompt, heads, D        units x blocks
-//   3 x 22 of 1000, 12/12, 64                         53064   20.0 -> 14.6
-//   8 x 8 of 500, 28/4, 128                           14592   21.2 ->  8.8
-//   16 x 16 of 1000, 28/4, 128                       121856   34.7 -> 23.2
-//   64 x 16 of 800, 28/4, 128                        258048   77.3 -> 57.7
-//   64 x 16 of 1800, 28/4, 128                       512000  105.7 -> 112.4
-//   128 x 4 of 500, 32/8, 64                         180224   40.6 -> 30.8
-//   16 x 16 of 1800, 32/8, 64                        256000   34.7 -> 39.5
+//   3 x 22 of 1000, 12/12, 64                         53064   19.7 -> 13.5
+//   8 x 8 of 500, 28/4, 128                           14592   21.1 ->  9.3
+//   16 x 16 of 1000, 28/4, 128                       121856   33.6 -> 21.7
+//   64 x 16 of 800, 28/4, 128                        258048   78.3 -> 54.6
+//   64 x 16 of 1800, 28/4, 128                       512000   98.7 -> 105.8
+//   128 x 4 of 500, 32/8, 64                         180224   40.3 -> 29.1
+//   16 x 16 of 1800, 32/8, 64                        256000   33.7 -> 34.2
+// The pages were in the last-level cache, which favours reading them often; so the
+// limits lie below the sizes where both take the same.
 int unit_waves_prefix(const sl_attn_desc *d, int kv, int num_groups)
 {
     const long long most = d->head_dim == 128 ? 400000 : 200000;

@@ -2,8 +2,16 @@
 // kernels of decode_split.hip and decode_shared.hip for FP4 records.
 //
 // Split-KV (split_fp4_kernel), with prefix sharing (prefix_fp4_kernel), and a
-// workgroup per unit for short sequences (unit_fp4_kernel). A step of the split
-// stream is four tiles (17 D bytes each, K and V), elsewhere two.
+// workgroup per unit for short sequences (unit_fp4_kernel). A step of the streams
+// is two or four tiles (step_tiles; 17 D bytes each, K and V).
+//
+// Measured (MI355X, split and merge, cold pages): 512 x 512 + lognormal(2048)
+// tokens, 28/4 heads of 128, 1.07 GB of records in 174 us, 6.2 TB/s (reading such
+// records at random without any arithmetic 6.7); 256 sequences of 64/8 heads, 2.26
+// GB in 350 us, 6.4 TB/s: bound by HBM. With head_dim 64 a record is half as long
+// for the same loads, scales and softmax: 384 x 1..2048, 32/8 heads, 0.21 GB in
+// 44.6 us, 4.6 TB/s, bound by instructions (VALU active for two thirds of the time
+// that a CU has work) and by the last workgroups' tail.
 #include "prefix_unit.h"
 
 namespace sl {
@@ -24,8 +32,8 @@ __global__ __launch_bounds__(kWave * kWavesPerBlock) void split_fp4_kernel(Split
 // query rows (members x heads of the largest sub-group with shared pages). With
 // four wavefronts per worker whatever the rows, those of the empty blocks stream
 // and compute for nothing: 8 prompts of 4000 tokens x 2 samples, 32/8 heads, D = 64
-// 31.8 -> 23.6 us; 16 of 4000 x 24, 12/12 heads, D = 64 115 -> 51; 64 of 2000 x 4,
-// 64/8 heads, D = 128 118 -> 79; with four blocks the same.
+// 31.8 -> 23.3 us; 16 of 4000 x 24, 12/12 heads, D = 64 115 -> 51; 64 of 2000 x 4,
+// 64/8 heads, D = 128 118 -> 76; with four blocks the same.
 // (Every wavefront looks for itself: two votes of the workgroup took 1 us.)
 __device__ __forceinline__ int shared_workers_per_block(const int32_t *s_sh, const int32_t *s_gl, int S, int group)
 {
@@ -103,7 +111,7 @@ __device__ __forceinline__ bool cut_short(const UnitGroups &g, const SplitParams
 // first product (length and table entries, then records and query rows). Bound by
 // that latency, and with thousands of units by instructions, as the stream is.
 // Steps of two tiles: with four, fewer workgroups fit a CU (384 x 1..1024, 32/8
-// heads, D = 64 29.6 us instead of 26.4; 512 x 1..256, 64/8 heads 40.5 and 26.0).
+// heads, D = 64 28.8 us instead of 25.5; 512 x 1..256, 64/8 heads 40.3 and 25.3).
 // With prefix sharing the members' rows of a prompt are attended one by one too
 // (its pages come out of the caches): the groups only decide which member is
 // shorter than its group's shared pages. A thread looks at one group, in the

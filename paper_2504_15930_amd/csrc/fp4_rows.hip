@@ -15,6 +15,11 @@
 // Eight elements per thread: a 16-byte load, four conversions
 // (v_cvt_scalef32_pk_fp4_bf16), and a 4-byte store of codes; a block is four
 // neighbouring threads, whose maximum takes two DPP moves.
+//
+// Bound by memory where there are many rows (the writer stores 68 bytes for 256
+// read, D = 128): 12322 tokens of 8 KV heads, 64 MB, in 15.5 us, 4.1 TB/s, read back
+// in 15.6 (a large copy: 5.1 TB/s); by the launch where there are few (96 rows 3.1
+// and 2.5 us).
 #include "fp4_unit.h"
 #include "wave_ops.h"
 

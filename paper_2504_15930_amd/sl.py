@@ -502,7 +502,8 @@ def _run_fp4(q, kv_pages, block_table, seq_lens, scale, groups, out, num_workers
 def decode_attn_fp4(q, kv_pages, block_table, seq_lens, scale, *, out=None, num_workers=0, workspace=None,
                     timing=None) -> torch.Tensor:
     """``sl_decode_attn_fp4``: decode attention over a 4-bit cache, ``kv_pages`` uint8
-    [num_pages, Hkv, ``fp4_record_bytes(D)``]; otherwise as ``decode_attn``."""
+    [num_pages, Hkv, ``fp4_record_bytes(D)``]; otherwise as ``decode_attn``. (Without ``workspace`` a captured call
+    uses the capturing stream's: graphs whose replays may overlap each need one of their own.)"""
     return _run_fp4(q, kv_pages, block_table, seq_lens, scale, None, out, num_workers, workspace, timing)
 
 
