@@ -191,13 +191,13 @@ int unit_waves(const sl_attn_desc *d, int kv)
 // 16-row blocks, the scans and a merge; attending every member by itself costs its
 // tiles again, out of the caches. Prefix kernel -> a workgroup per unit:
 //   prompts x samples of prompt, heads, D        units x blocks
-//   3 x 22 of 1000, 12/12, 64                         53064   19.7 -> 13.5
+//   3 x 22 of 1000, 12/12, 64                         53064   16.4 -> 12.8
 //   8 x 8 of 500, 28/4, 128                           14592   21.1 ->  9.3
 //   16 x 16 of 1000, 28/4, 128                       121856   33.6 -> 21.7
 //   64 x 16 of 800, 28/4, 128                        258048   78.3 -> 54.6
 //   64 x 16 of 1800, 28/4, 128                       512000   98.7 -> 105.8
-//   128 x 4 of 500, 32/8, 64                         180224   40.3 -> 29.1
-//   16 x 16 of 1800, 32/8, 64                        256000   33.7 -> 34.2
+//   128 x 4 of 500, 32/8, 64                         180224   37.1 -> 28.6
+//   16 x 16 of 1800, 32/8, 64                        256000   31.5 -> 33.9
 // The pages were in the last-level cache, which favours reading them often; so the
 // limits lie below the sizes where both take the same.
 int unit_waves_prefix(const sl_attn_desc *d, int kv, int num_groups)

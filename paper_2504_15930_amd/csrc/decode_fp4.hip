@@ -3,15 +3,15 @@
 //
 // Split-KV (split_fp4_kernel), with prefix sharing (prefix_fp4_kernel), and a
 // workgroup per unit for short sequences (unit_fp4_kernel). A step of the streams
-// is two or four tiles (step_tiles; 17 D bytes each, K and V).
+// is four tiles, with prefix sharing two (17 D bytes each, K and V).
 //
 // Measured (MI355X, split and merge, cold pages): 512 x 512 + lognormal(2048)
 // tokens, 28/4 heads of 128, 1.07 GB of records in 174 us, 6.2 TB/s (reading such
 // records at random without any arithmetic 6.7); 256 sequences of 64/8 heads, 2.26
 // GB in 350 us, 6.4 TB/s: bound by HBM. With head_dim 64 a record is half as long
 // for the same loads, scales and softmax: 384 x 1..2048, 32/8 heads, 0.21 GB in
-// 44.6 us, 4.6 TB/s, bound by instructions (VALU active for two thirds of the time
-// that a CU has work) and by the last workgroups' tail.
+// 44.6 us, 4.6 TB/s, the VALUs busy for 40% of it; at the end the CUs run out of
+// workgroups one by one (a CU has work for three quarters of the time).
 #include "prefix_unit.h"
 
 namespace sl {
@@ -32,8 +32,8 @@ __global__ __launch_bounds__(kWave * kWavesPerBlock) void split_fp4_kernel(Split
 // query rows (members x heads of the largest sub-group with shared pages). With
 // four wavefronts per worker whatever the rows, those of the empty blocks stream
 // and compute for nothing: 8 prompts of 4000 tokens x 2 samples, 32/8 heads, D = 64
-// 31.8 -> 23.3 us; 16 of 4000 x 24, 12/12 heads, D = 64 115 -> 51; 64 of 2000 x 4,
-// 64/8 heads, D = 128 118 -> 76; with four blocks the same.
+// 31.8 -> 20.0 us; 16 of 4000 x 24, 12/12 heads, D = 64 115 -> 48; 64 of 2000 x 4,
+// 64/8 heads, D = 128 118 -> 74; with four blocks the same.
 // (Every wavefront looks for itself: two votes of the workgroup took 1 us.)
 __device__ __forceinline__ int shared_workers_per_block(const int32_t *s_sh, const int32_t *s_gl, int S, int group)
 {

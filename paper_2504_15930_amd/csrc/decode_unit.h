@@ -70,15 +70,17 @@ namespace {
 //   E4M3 D = 128, 512 x 512 + lognormal(2048)        319 -> 316 us; at 768 workers 381 -> 327
 //   E4M3 D = 64, 384 x 1..4096 tokens, 8 KV heads   226 -> 146 us (two tiles: 157)
 // FP4: four tiles per step carry as much as two of E4M3 (two per step: 512 x 512 +
-// lognormal(2048), 28/4 heads, 191 us instead of 172), but not in the prefix
-// kernel of D = 128, where the registers of four leave no room for a shared-page
-// workgroup beside an own-page one (32 prompts x 8 samples, 59 us instead of 43).
+// lognormal(2048), 28/4 heads, 191 us instead of 174), but not in the prefix
+// kernel, where the registers of four leave no room for a shared-page workgroup
+// beside an own-page one (D = 128, 32 prompts of 1024 x 8 samples, 28/4 heads, 59
+// us instead of 43) or for a second one (D = 64, 32 prompts of 4000 x 8, 32/8
+// heads, 59 instead of 56; 8 of 4000 x 2, 23 instead of 20).
 // Two steps in flight; three were no faster anywhere (and slower where they
 // cost a resident workgroup, in the prefix kernel).
 template <int D, int KV, bool PREFIX = false>
 constexpr int step_tiles()
 {
-    return is_fp4(KV) ? (PREFIX && D == 128 ? 2 : 4) : D == 64 ? (KV == kE4m3 ? 4 : 2) : (KV == kE4m3 ? 2 : 1);
+    return is_fp4(KV) ? (PREFIX ? 2 : 4) : D == 64 ? (KV == kE4m3 ? 4 : 2) : (KV == kE4m3 ? 2 : 1);
 }
 constexpr int kPipelineDepth = 2;
 // Four E4M3 codes (one dword) -> four bf16 (two dwords), exact.
