@@ -254,11 +254,13 @@ __global__ __launch_bounds__(kPageThreads) void release_pages_kernel(PageParams 
     }
 }
 
-// Entries of the slot map, or of the block table, per workgroup, at least: below
-// four per thread the scans, which every workgroup repeats, would be most of its
-// work. Workgroups at most, one per CU.
-constexpr uint32_t kItemsPerBlock = 4 * kPageThreads;
+// Entries of the slot map, or of the block table, per workgroup, at least: one per
+// thread (66000 tokens of 96 requests 5.7 us, with four 8.4). Workgroups at most, one per
+// CU. Where one workgroup has to do everything, it makes the slot map too up to
+// this many entries.
+constexpr uint32_t kItemsPerBlock = kPageThreads;
 constexpr uint32_t kMostBlocks = 256;
+constexpr uint32_t kAloneSlots = 4 * kPageThreads;
 
 // Neither the lengths nor the count is updated in place.
 bool apart(const PageParams &p) { return p.seq_lens_out != p.seq_lens && p.free_count_out != p.free_count; }
@@ -267,13 +269,13 @@ bool apart(const PageParams &p) { return p.seq_lens_out != p.seq_lens && p.free_
 
 // (One request per thread where that is enough: the code for eight is four times
 // as long, and a first pass through it is instruction fetches.)
-// Call with 1024 requests of 1000 tokens: 11.8 us, with one workgroup for the
-// pages and a second launch 65; 96 of 1365: 11.8 and 14.6; 8192 of 100: 24 and 92.
+// Call with 1024 requests of 1000 tokens: 11.4 us, with one workgroup for the
+// pages and a second launch 65; 96 of 1365: 11.2 and 14.6; 8192 of 100: 24 and 92.
 hipError_t launch_extend_pages(const PageParams &p, hipStream_t stream)
 {
     const uint32_t tokens = (uint32_t)p.max_tokens;
-    const uint32_t each = std::max(kItemsPerBlock, (tokens + kMostBlocks - 1) / kMostBlocks);
-    const bool one_launch = apart(p) || tokens <= kItemsPerBlock;
+    const uint32_t each = apart(p) ? std::max(kItemsPerBlock, (tokens + kMostBlocks - 1) / kMostBlocks) : kAloneSlots;
+    const bool one_launch = apart(p) || tokens <= kAloneSlots;
     const uint32_t blocks = one_launch && tokens > 0 ? (tokens + each - 1) / each : 1;
     hipLaunchKernelGGL(p.batch <= kPageThreads ? extend_pages_kernel<1> : extend_pages_kernel<kMostPer>, dim3(blocks),
                        dim3(kPageThreads), sizeof(uint32_t) * (3 * (size_t)p.batch + 2), stream, p,
