@@ -318,7 +318,8 @@ sl_status sl_kv_append_fp4(const sl_attn_desc *desc, const uint16_t *k_new, cons
  * page * 16 + slot in the page (a slot map as sl_pages_extend makes it), for
  * every KV head. sl_kv_write_fp4 quantises num_tokens rows into the cache, as
  * prefill does with a chunk of prompts; sl_kv_read_fp4 returns rows as bf16, the
- * stored values exactly, for a dense kernel over earlier tokens.
+ * stored values exactly (2^128 and more, which only records written elsewhere
+ * hold, as infinities), for a dense kernel over earlier tokens.
  *   k_new, v_new, k_out, v_out  bf16 bits [num_tokens][Hkv][D], 16-byte aligned
  *   slots                       device int32 [num_tokens]
  * A negative slot is no token: nothing is written, and zero rows are read. A slot
@@ -367,7 +368,10 @@ sl_status sl_kv_read_fp4(const sl_attn_desc *desc, const uint8_t *kv_pages, cons
  * the stack, request by request and a request's last block first, and sets its
  * length to 0 (a request whose length is invalid is left as it is; pages beyond
  * num_pages in all, which a request released twice brings, are dropped). The
- * block table is not changed.
+ * block table is not changed. A page belongs to one request here: one that several
+ * rows of the block table name, as with prefix sharing, would come back once for
+ * each, so its owner keeps such pages out of the released rows (a table and
+ * lengths of the members' own blocks) and releases them as a request of their own.
  *
  * Other than the aliases named, the arrays must not overlap. Both use desc fields
  * batch (also 0), page_size, max_blocks_per_seq, num_pages and stream; no

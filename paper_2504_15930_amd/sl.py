@@ -622,7 +622,8 @@ def pages_extend(seq_lens, new_tokens, block_table, free_pages, free_count, max_
 
 def pages_release(finished, seq_lens, block_table, free_pages, free_count, *, seq_lens_out=None, free_count_out=None):
     """``sl_pages_release``: the pages of requests with ``finished`` [B] not 0 go back on the stack, in place, and
-    their lengths become 0. Returns ``(seq_lens_out, free_count_out)``, which may be the inputs themselves."""
+    their lengths become 0. Returns ``(seq_lens_out, free_count_out)``, which may be the inputs themselves. A page that
+    several rows share would come back once for each: keep such pages out of the released rows."""
     try:
         (B,), blocks, (N,), index = seq_lens.shape, block_table.shape[1], free_pages.shape, seq_lens.get_device()
     except _BAD_SIZES:

@@ -73,6 +73,27 @@ def test_write_and_read(T, Hkv, D):
         assert np.array_equal(got.float().cpu().double().numpy(), ref, equal_nan=True)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_every_code_under_every_scale_byte(D):
+    """Records that others wrote: all 16 codes under all 256 scale bytes, read back as they are defined; bf16 holds
+    each of them but those of 2^128 and beyond, which are infinite in it."""
+    T, C = 256, D // 32
+    k, v, shift, ks, vs = fp4.layout(D)
+    pool = np.zeros((T // 16, 1, 17 * D), np.uint8)
+    codes = (np.arange(D) + np.arange(T)[:, None]) % 16
+    for t in range(T):
+        rec = pool[t // 16, 0]
+        for at, at_scale in ((k, ks), (v, vs)):
+            rec[at[t % 16, ::2]] = codes[t, ::2] | codes[t, 1::2] << 4
+            rec[at_scale[t % 16]] = (t + 85 * np.arange(C)) % 256
+    got = sl.kv_read_fp4(torch.arange(T, dtype=torch.int32, device=DEV), torch.from_numpy(pool).to(DEV))
+    torch.cuda.synchronize()
+    want = fp4.values(codes, ((np.arange(T)[:, None] + 85 * np.arange(C)) % 256).astype(np.uint8))
+    want = np.where(np.abs(want) >= 2.0 ** 128, np.copysign(np.inf, want), want)
+    for x in got:
+        assert np.array_equal(x[:, 0].float().cpu().double().numpy(), want, equal_nan=True)
+
+
 def test_whole_pages_in_order():
     """A prompt's rows in slot order, pages scattered, the last one partly filled."""
     rng = np.random.default_rng(8)
