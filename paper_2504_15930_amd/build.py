@@ -1,6 +1,6 @@
-"""Build ``libsl.so`` (the gfx950 HIP kernels plus the C ABI) in-tree with hipcc.
+"""Build ``libsl.so`` (the gfx950 HIP kernels plus the C ABI) in-tree with hipcc, and ``_binding.so`` beside it.
 
-Every call compiles from scratch; the library lands next to this file.
+Every call compiles from scratch; the libraries land next to this file.
 """
 from __future__ import annotations
 
@@ -14,6 +14,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIBRARY = os.path.join(HERE, "libsl.so")
+BINDING = os.path.join(HERE, "_binding.so")
 SOURCES = ["decode_split.hip", "decode_shared.hip", "decode_fp4.hip", "merge.hip", "append.hip", "fp4_rows.hip", "pages.hip", "engine.hip", "api.cpp",
            "engine.cpp", "dispatch.cpp", "noalloc.hip"]
 ARCH = "gfx950"
@@ -35,6 +36,24 @@ def _hipcc() -> str:
     return os.path.join(rocm, "bin", "hipcc")
 
 
+def build_binding(output: str = BINDING) -> str:
+    """Compile csrc/binding.cpp, the Python entry points that read torch's tensors directly (host code only)."""
+    import sysconfig
+
+    import torch
+
+    root, rocm = os.path.dirname(torch.__file__), os.environ.get("ROCM_PATH", "/opt/rocm")
+    tmp = output + ".tmp%d" % os.getpid()
+    subprocess.run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+                    f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                    "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"],
+                    *(x for d in ("include", "include/torch/csrc/api/include") for x in ("-isystem", os.path.join(root, d))),
+                    "-isystem", os.path.join(rocm, "include"), os.path.join(CSRC, "binding.cpp"), "-o", tmp,
+                    "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_hip", "-lc10"], check=True)
+    os.replace(tmp, output)
+    return output
+
+
 def build(output: str = LIBRARY, extra: list[str] | None = None, verbose: bool = False,
           objdir: str | None = None) -> str:
     """Compile every source and link ``output``; returns its path."""
@@ -51,8 +70,11 @@ def build(output: str = LIBRARY, extra: list[str] | None = None, verbose: bool =
         subprocess.run(cmd, check=True)
         return obj
 
-    with ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    with ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        binding = ex.submit(build_binding) if output == LIBRARY else None   # (another build's library is called by it too)
         objs = list(ex.map(compile_one, SOURCES))
+        if binding:
+            binding.result()
     tmp = output + ".tmp%d" % os.getpid()
     cmd = [_hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", *objs, "-o", tmp]
     if verbose:
