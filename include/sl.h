@@ -88,13 +88,15 @@ typedef struct sl_attn_desc {
     int32_t num_pages;          /* pages in each pool; valid page ids are [0, num_pages) */
     int32_t num_workers;        /* split-KV workers (wavefronts). 0: library default
                                    (three per CU for a bf16 cache with head_dim 128, eight
-                                   for a 4-bit one with head_dim 64, else, and for
-                                   prefix-shared attention, four per CU; none with a 4-bit
-                                   cache and at most 128 blocks per sequence, a workgroup
-                                   per sequence and KV head, unless prefix sharing saves
-                                   more);
-                                   1..65536: exactly this many. The result does not depend on it beyond fp32
-                                   rounding; tests vary it to exercise the merge. */
+                                   for a 4-bit one with head_dim 64 and more than 128
+                                   sequences x KV heads, three for one with head_dim 128
+                                   and at most 32, else, and for prefix-shared attention,
+                                   four per CU; none with a 4-bit cache and at most 128
+                                   blocks per sequence, a workgroup per sequence and KV
+                                   head, unless prefix sharing saves more);
+                                   1..65536: exactly this many. The result does not depend
+                                   on it beyond fp32 rounding; tests vary it to exercise
+                                   the merge. */
     hipStream_t stream;         /* stream the work is enqueued on (0: null stream) */
     void *workspace;            /* device scratch, >= sl_decode_attn_workspace_size bytes,
                                    256-byte aligned; contents need no initialisation */

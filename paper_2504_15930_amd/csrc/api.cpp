@@ -146,12 +146,20 @@ sl_status resolve_workers(const sl_attn_desc *d, int kv, int *nw, bool prefix = 
     // sequences of 1..2048 tokens, 32/8 heads: 52.4 us, with one 60.7). With head_dim
     // 128 two were slower (512 x 512 + lognormal(2048), 28/4 heads: 174 us with one,
     // 187 with two; 256 of 64/8 heads 350 and 367).
+    // With few units (sequences x KV heads) the merge of every worker's pieces weighs more than
+    // the last workers' share of the stream: up to 32 units three workgroups per four CUs take
+    // less with head_dim 128 (4 x 1..16384 tokens, 28/4 heads 18.5 -> 17.0 us, 2 of 64/8 18.1 ->
+    // 16.3; at 40 and 64 units the same), up to 128 units one per CU with head_dim 64 (1 x 1..8192,
+    // 32/8 heads 12.3 -> 10.6, 16 of them 18.0 -> 17.0; 32 of them 24.4 -> 26.9).
     // Prefix-shared attention keeps one own-page workgroup per CU beside its shared-page
     // workgroups (three per four CUs was 12% slower).
     const int blocks = info->blocks[d->head_dim == 128][kv];
-    const int per_cu4 = kv == kFp4 && !prefix && d->head_dim == 64 && blocks > 1 ? 8   // workgroups per four CUs
-                        : kv != kBf16 || prefix || d->head_dim == 64             ? 4
-                                                                                 : 3;
+    const long long units = (long long)d->batch * d->num_kv_heads;
+    int per_cu4 = kv != kBf16 || prefix || d->head_dim == 64 ? 4 : 3;   // workgroups per four CUs
+    if (kv == kFp4 && !prefix && d->head_dim == 64 && blocks > 1 && units > 128)
+        per_cu4 = 8;
+    if (kv == kFp4 && !prefix && d->head_dim == 128 && units <= 32)
+        per_cu4 = 3;
     *nw = (blocks > 0 ? info->cus * per_cu4 / 4 : info->cus) * kWavesPerBlock;
     if (*nw > kMaxWorkers)
         *nw = kMaxWorkers;
@@ -169,8 +177,8 @@ int shared_workers(int nw) { return nw / 4 > 0 ? nw / 4 : 1; }
 // Wavefronts per unit if plain attention over a 4-bit cache runs as one workgroup
 // per unit (launch_unit_fp4), else 0: where the block table says that every
 // sequence is short. (The lengths themselves are not known here; a call with a
-// worker count of its own gets the workers.) Eight where that leaves every
-// workgroup a CU. Calls, split and merge -> a workgroup per unit, MI355X, tokens
+// worker count of its own gets the workers.) Eight where the table is long and that
+// leaves every workgroup a CU. Calls, split and merge -> a workgroup per unit, MI355X, tokens
 // 1 .. 16 times the table's blocks:
 //   blocks                 16             64            128               256
 //   5 x 28/4 heads                   13.0 ->  8.0   12.4 ->  9.3
@@ -179,12 +187,14 @@ int shared_workers(int nw) { return nw / 4 > 0 ? nw / 4 : 1; }
 //   512 x 64/8         36.4 -> 25.3  73.3 -> 56.7
 //   384 x 32/8, D = 64 20.1 -> 12.9  35.8 -> 25.5   53.2 -> 44.4   92.0 -> 87.0
 //   4 x 32/8, D = 64                                               12.9 -> 14.5
-// (512 x 64/8 of 16 blocks with eight wavefronts 42.6, 64 x 28/4 of 128 with four 13.4.)
+// (512 x 64/8 of 16 blocks with eight wavefronts 42.6; up to 64 blocks eight gain nothing: 64 x 28/4 of 64
+// 8.6 and with four 8.5, 64 x 32/8, D = 64 of 48 8.2 and 7.6, 8 x 4/2, D = 64 of 16 4.8 and 4.4; of 128
+// blocks 64 x 28/4 11.7 and 12.7, 5 x 28/4 9.7 and 10.4.)
 int unit_waves(const sl_attn_desc *d, int kv)
 {
     if (kv != kFp4 || d->num_workers != 0 || d->max_blocks_per_seq > kUnitBlocks)
         return 0;
-    return (long long)d->batch * d->num_kv_heads <= 256 ? 8 : 4;
+    return (long long)d->batch * d->num_kv_heads <= 256 && d->max_blocks_per_seq > 64 ? 8 : 4;
 }
 
 // The same for prefix sharing. Reading the shared pages once costs the products of
