@@ -104,6 +104,74 @@ __device__ __forceinline__ bool cut_short(const UnitGroups &g, const SplitParams
     return true;
 }
 
+// The sequence that is number `turn` when those of the longest quarter of the
+// table's width come first, then the next quarter, and so on, in batch order
+// within each; its length in L. Every wavefront votes on its 64 sequences of every
+// pass over the batch, one mask per quarter; the masks lie in turn order, a lane of
+// each wavefront has one, and a scan of their counts says which holds `turn`. Ends
+// without a barrier (the arrays are its own).
+template <int PASSES>
+struct TurnLds {
+    uint64_t mask[4][PASSES][kWavesPerBlock];
+    int32_t len[PASSES * kWavesPerBlock * kWave];
+};
+struct TurnSum {
+    static constexpr int kIdentity = 0;
+    __device__ static int op(int a, int b) { return a + b; }
+};
+template <int PASSES>
+__device__ __forceinline__ int sequence_in_turn(TurnLds<PASSES> &s, const SplitParams &p, int turn, int wave, int lane,
+                                                int &L)
+{
+    static_assert(4 * PASSES * kWavesPerBlock == kWave, "a mask per lane");
+    constexpr int kThreads = kWavesPerBlock * kWave;
+    int len[PASSES];
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+        const int b = i * kThreads + (int)threadIdx.x;
+        len[i] = b < p.batch ? p.seq_lens[b] : 0;
+    }
+    const int width = p.max_blocks * (kPageSize / 4);   // a quarter of the table, in tokens
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+        const int b = i * kThreads + (int)threadIdx.x;
+        const int shorter = (len[i] <= width) + (len[i] <= 2 * width) + (len[i] <= 3 * width);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const uint64_t mask = __builtin_amdgcn_ballot_w64(b < p.batch && shorter == c);
+            if (lane == 0)
+                s.mask[c][i][wave] = mask;
+        }
+        s.len[b] = len[i];
+    }
+    __syncthreads();
+    const uint64_t mask = (&s.mask[0][0][0])[lane];
+    const int count = __builtin_popcountll(mask), upto = wave_scan<TurnSum>(count);
+    const uint64_t holder = __builtin_amdgcn_ballot_w64(upto - count <= turn && turn < upto);   // one lane
+    const int at = __builtin_ctzll(holder);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)mask, at),
+                   hi = (uint32_t)__builtin_amdgcn_readlane((int)(mask >> 32), at);
+    const int rank = turn - __builtin_amdgcn_readlane(upto - count, at);
+    const bool here = (((uint64_t)hi << 32 | lo) >> lane & 1) != 0 &&
+                      (int)__builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0)) == rank;
+    const int b = at % (PASSES * kWavesPerBlock) / kWavesPerBlock * kThreads + at % kWavesPerBlock * kWave +
+                  __builtin_ctzll(__builtin_amdgcn_ballot_w64(here));
+    L = __builtin_amdgcn_readfirstlane(s.len[b]);
+    return b;
+}
+// Where it is done: with long tables and more units than CUs. It costs 0.5 to 1 us
+// of a call, and the long sequences that would start last no longer run alone at the
+// end (calls in batch order -> in turn, cold pages, tokens 1 .. 16 times the table):
+//   130 x 28/4 heads of 128, 128 blocks     23.6 -> 19.4    96 of them    16.8 -> 15.6
+//   300 x 32/2 of 128, 128 blocks           25.0 -> 22.1    all of 12 tokens per block 27.3 -> 28.0
+//   384 x 32/8 of 64, 128 blocks            47.8 -> 46.1    all of 12     57.7 -> 58.7
+//   600 x 32/2 of 64, 80 blocks             18.5 -> 17.0    lognormal     13.1 -> 12.2
+//   256 x 28/4 of 128, 64 blocks            17.9 -> 18.8    512 x 64/8 of 16 blocks    26.0 -> 31.8
+// Not with prefix sharing, whose members read a prompt's pages side by side.
+constexpr int kTurnUnits = 256, kTurnBlocks = 64;
+constexpr int kTurnPasses = 4;
+constexpr int kTurnBatch = kTurnPasses * kWavesPerBlock * kWave;
+
 // Attention where every sequence is short (a block table of at most
 // kUnitBlocks entries): one workgroup per unit, its tiles dealt to the wavefronts
 // in contiguous runs of whole steps, their states combined in LDS. One launch, no
@@ -116,7 +184,7 @@ __device__ __forceinline__ bool cut_short(const UnitGroups &g, const SplitParams
 // (its pages come out of the caches): the groups only decide which member is
 // shorter than its group's shared pages. A thread looks at one group, in the
 // first trip to memory.
-template <int D, int KV, int WAVES>
+template <int D, int KV, int WAVES, bool TURNS>
 __global__ __launch_bounds__(kWave * WAVES) void unit_fp4_kernel(SplitParams p, UnitGroups groups)
 {
     constexpr int NT = kUnitStepTiles;
@@ -124,11 +192,19 @@ __global__ __launch_bounds__(kWave * WAVES) void unit_fp4_kernel(SplitParams p, 
     // Per wavefront what stage_partial writes: G rows of D fp32, then G pairs (m, l).
     __shared__ __attribute__((aligned(16))) uint8_t s_state[WAVES][(HALF ? 8 : kMaxGroup) * (D + 2) * 4];
     const int G = p.group, Hkv = p.num_kv_heads;
-    const int unit = blockIdx.x, b = unit / Hkv, g = unit - b * Hkv;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x & (kWave - 1);
+    const int turn = blockIdx.x / Hkv, g = blockIdx.x - turn * Hkv;
+    int b = turn, L;
+    if constexpr (TURNS) {
+        static_assert(WAVES == kWavesPerBlock, "the threads of sequence_in_turn");
+        __shared__ TurnLds<kTurnPasses> s_turn;
+        b = sequence_in_turn(s_turn, p, turn, wave, lane, L);
+    } else {
+        L = p.seq_lens[b];
+    }
+    const int unit = b * Hkv + g;
     const int n = lane & 15, quad = lane >> 4;
     const int max_len = p.max_blocks * kPageSize;
-    const int L = p.seq_lens[b];
     const int pages = pages_of(L, max_len), steps = (pages + NT - 1) / NT;
     const int first = wave * steps / WAVES, count = (wave + 1) * steps / WAVES - first;
     const int tiles = min(count * NT, pages - first * NT);   // this wavefront's, at most kWave
@@ -214,13 +290,13 @@ __global__ __launch_bounds__(kWave * WAVES) void unit_fp4_kernel(SplitParams p, 
 }  // namespace
 
 namespace {
-template <int WAVES>
+template <int WAVES, bool TURNS>
 UnitKernel unit_kernel(int head_dim, int group)
 {
     if (head_dim == 128)
-        return group <= 8 ? unit_fp4_kernel<128, kFp4Half, WAVES> : unit_fp4_kernel<128, kFp4, WAVES>;
+        return group <= 8 ? unit_fp4_kernel<128, kFp4Half, WAVES, TURNS> : unit_fp4_kernel<128, kFp4, WAVES, TURNS>;
     if (head_dim == 64)
-        return group <= 8 ? unit_fp4_kernel<64, kFp4Half, WAVES> : unit_fp4_kernel<64, kFp4, WAVES>;
+        return group <= 8 ? unit_fp4_kernel<64, kFp4Half, WAVES, TURNS> : unit_fp4_kernel<64, kFp4, WAVES, TURNS>;
     return nullptr;
 }
 }  // namespace
@@ -228,10 +304,15 @@ UnitKernel unit_kernel(int head_dim, int group)
 hipError_t launch_unit_fp4(const SplitParams &p, const UnitGroups &groups, int waves, int head_dim,
                            hipStream_t stream)
 {
-    const UnitKernel kernel = waves == 8 ? unit_kernel<8>(head_dim, p.group) : unit_kernel<4>(head_dim, p.group);
+    const int units = p.batch * p.num_kv_heads;
+    const bool turns = waves == kWavesPerBlock && groups.count == 0 && units > kTurnUnits && p.max_blocks > kTurnBlocks &&
+                       p.batch <= kTurnBatch;
+    const UnitKernel kernel = turns        ? unit_kernel<kWavesPerBlock, true>(head_dim, p.group)
+                              : waves == 8 ? unit_kernel<8, false>(head_dim, p.group)
+                                           : unit_kernel<4, false>(head_dim, p.group);
     if (!kernel)
         return hipErrorInvalidValue;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.batch * p.num_kv_heads)), dim3(kWave * waves), 0, stream, p, groups);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)units), dim3(kWave * waves), 0, stream, p, groups);
     return hipGetLastError();
 }
 

@@ -206,6 +206,35 @@ def test_table_widths(B, hq, hkv, d, blocks):
     assert torch.equal(again[3:], out[3:])
 
 
+@pytest.mark.parametrize("B,blocks", [(129, 65), (256, 128), (257, 65), (511, 66), (513, 65), (1024, 65), (1025, 65)])
+@pytest.mark.parametrize("law", ["edges", "equal", "empty"])
+def test_every_sequence_in_its_turn(B, blocks, law):
+    """More units than CUs over long tables, where the longer sequences are started first: every sequence is attended
+    once, whatever quarters of the table's width their lengths lie in."""
+    _say("turns", B, blocks, law)
+    rng = np.random.default_rng(B)
+    edges = [x for q in (0, 4 * blocks, 8 * blocks, 12 * blocks, 16 * blocks) for x in (q - 1, q, q + 1)
+             if 0 <= x <= 16 * blocks]
+    L = {"edges": rng.choice(edges, B), "equal": np.full(B, 100), "empty": np.zeros(B, np.int64)}[law]
+    L[int(rng.integers(B))] = 16 * blocks
+    b, pool = make(L, 4, 2, 64, seed=B)
+    out = sl.decode_attn_fp4(b.q, pool, b.block_table, b.seq_lens, b.scale)
+    torch.cuda.synchronize()
+    assert b.block_table.shape[1] == blocks
+    rows = sorted({0, 1, B // 2, B - 2, B - 1, int(L.argmax()), *rng.integers(0, B, 20).tolist()})
+    assert_parity(out[rows], reference(b, pool, rows), f"{B} x {blocks} {law}")
+    split = sl.decode_attn_fp4(b.q, pool, b.block_table, b.seq_lens, b.scale, num_workers=512)
+    # (both within the tolerance of the oracle: within twice of one another)
+    assert ((out.float() - split.float()).abs() <= 2e-2 + 4e-2 * split.float().abs()).all()
+    lens = b.seq_lens.clone()
+    bad = [0, B // 2]
+    lens[bad[0]], lens[bad[1]] = -1, 2 ** 31 - 1
+    again = sl.decode_attn_fp4(b.q, pool, b.block_table, lens, b.scale)
+    torch.cuda.synchronize()
+    keep = [i for i in range(B) if i not in bad]
+    assert torch.isnan(again[bad]).all() and torch.equal(again[keep], out[keep])
+
+
 @pytest.mark.parametrize("scale", [-0.3, 0.0, 1e-3, 30.0])
 @pytest.mark.parametrize("workers", [0, 5])
 def test_scales(scale, workers):
