@@ -49,7 +49,7 @@ def build_binding(output: str = BINDING) -> str:
                     "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_paths()["include"],
                     *(x for d in ("include", "include/torch/csrc/api/include") for x in ("-isystem", os.path.join(root, d))),
                     "-isystem", os.path.join(rocm, "include"), os.path.join(CSRC, "binding.cpp"), "-o", tmp,
-                    "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10_hip", "-lc10"], check=True)
+                    "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch_hip", "-lc10_hip", "-lc10"], check=True)
     os.replace(tmp, output)
     return output
 
