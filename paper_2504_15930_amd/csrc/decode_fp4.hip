@@ -10,8 +10,7 @@
 // records at random without any arithmetic 6.7); 256 sequences of 64/8 heads, 2.26
 // GB in 350 us, 6.4 TB/s: bound by HBM. With head_dim 64 a record is half as long
 // for the same loads, scales and softmax: 384 x 1..2048, 32/8 heads, 0.21 GB in
-// 44.6 us, 4.6 TB/s, the VALUs busy for 40% of it; at the end the CUs run out of
-// workgroups one by one (a CU has work for three quarters of the time).
+// 42.3 us, 4.9 TB/s, the VALUs busy for half of it.
 #include "prefix_unit.h"
 
 namespace sl {
@@ -123,29 +122,34 @@ template <int PASSES>
 __device__ __forceinline__ int sequence_in_turn(TurnLds<PASSES> &s, const SplitParams &p, int turn, int wave, int lane,
                                                 int &L)
 {
-    static_assert(4 * PASSES * kWavesPerBlock == kWave, "a mask per lane");
+    constexpr int kMasks = 4 * PASSES * kWavesPerBlock;
+    static_assert(kMasks <= kWave, "a mask per lane");
     constexpr int kThreads = kWavesPerBlock * kWave;
     int len[PASSES];
 #pragma unroll
-    for (int i = 0; i < PASSES; ++i) {
-        const int b = i * kThreads + (int)threadIdx.x;
-        len[i] = b < p.batch ? p.seq_lens[b] : 0;
-    }
+    for (int i = 0; i < PASSES; ++i)
+        if (i * kThreads < p.batch)
+            len[i] = p.seq_lens[min(i * kThreads + (int)threadIdx.x, p.batch - 1)];
     const int width = p.max_blocks * (kPageSize / 4);   // a quarter of the table, in tokens
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) {
+        if (i * kThreads >= p.batch) {
+            if (lane < 4)
+                s.mask[lane][i][wave] = 0;
+            continue;
+        }
         const int b = i * kThreads + (int)threadIdx.x;
-        const int shorter = (len[i] <= width) + (len[i] <= 2 * width) + (len[i] <= 3 * width);
+        const int quarter = b < p.batch ? (len[i] <= width) + (len[i] <= 2 * width) + (len[i] <= 3 * width) : -1;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-            const uint64_t mask = __builtin_amdgcn_ballot_w64(b < p.batch && shorter == c);
+            const uint64_t mask = __builtin_amdgcn_ballot_w64(quarter == c);
             if (lane == 0)
                 s.mask[c][i][wave] = mask;
         }
         s.len[b] = len[i];
     }
     __syncthreads();
-    const uint64_t mask = (&s.mask[0][0][0])[lane];
+    const uint64_t mask = lane < kMasks ? (&s.mask[0][0][0])[lane] : 0;
     const int count = __builtin_popcountll(mask), upto = wave_scan<TurnSum>(count);
     const uint64_t holder = __builtin_amdgcn_ballot_w64(upto - count <= turn && turn < upto);   // one lane
     const int at = __builtin_ctzll(holder);
@@ -159,17 +163,20 @@ __device__ __forceinline__ int sequence_in_turn(TurnLds<PASSES> &s, const SplitP
     L = __builtin_amdgcn_readfirstlane(s.len[b]);
     return b;
 }
-// Where it is done: with long tables and more units than CUs. It costs 0.5 to 1 us
-// of a call, and the long sequences that would start last no longer run alone at the
-// end (calls in batch order -> in turn, cold pages, tokens 1 .. 16 times the table):
-//   130 x 28/4 heads of 128, 128 blocks     23.6 -> 19.4    96 of them    16.8 -> 15.6
-//   300 x 32/2 of 128, 128 blocks           25.0 -> 22.1    all of 12 tokens per block 27.3 -> 28.0
-//   384 x 32/8 of 64, 128 blocks            47.8 -> 46.1    all of 12     57.7 -> 58.7
-//   600 x 32/2 of 64, 80 blocks             18.5 -> 17.0    lognormal     13.1 -> 12.2
-//   256 x 28/4 of 128, 64 blocks            17.9 -> 18.8    512 x 64/8 of 16 blocks    26.0 -> 31.8
-// Not with prefix sharing, whose members read a prompt's pages side by side.
+// Where it is done: with long tables and more units than CUs, up to two passes. It costs
+// some 0.5 us of a call, and the long sequences that would start last no longer run alone
+// at the end. Calls in batch order -> in turn, cold pages, tokens 1 .. 16 times the table
+// (all of 12 tokens per block):
+//   96 x 28/4 heads of 128, 128 blocks   16.8 -> 15.1 (17.2 -> 17.6)    130 of them 23.6 -> 18.9
+//   300 x 32/2 of 128, 128 blocks        25.0 -> 21.8 (27.3 -> 27.8)
+//   384 x 32/8 of 64, 128 blocks         47.8 -> 45.7 (58.4 -> 58.5)
+//   150 x 32/8 of 64, 80 blocks          16.2 -> 15.1 (18.1 -> 18.4)
+// Not so with shorter tables (256 x 28/4 of 128, 64 blocks 18.1 -> 18.4, 300 x 32/8 of 64, 32
+// blocks 15.1 -> 15.8) and with four passes (1000 x 28/4 of 128, 100 blocks 81.6 -> 82.0,
+// lognormal lengths 43.0 -> 46.1). Nor with prefix sharing, whose members read a prompt's
+// pages side by side.
 constexpr int kTurnUnits = 256, kTurnBlocks = 64;
-constexpr int kTurnPasses = 4;
+constexpr int kTurnPasses = 2;
 constexpr int kTurnBatch = kTurnPasses * kWavesPerBlock * kWave;
 
 // Attention where every sequence is short (a block table of at most

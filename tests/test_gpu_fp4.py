@@ -206,7 +206,7 @@ def test_table_widths(B, hq, hkv, d, blocks):
     assert torch.equal(again[3:], out[3:])
 
 
-@pytest.mark.parametrize("B,blocks", [(129, 65), (256, 128), (257, 65), (511, 66), (513, 65), (1024, 65), (1025, 65)])
+@pytest.mark.parametrize("B,blocks", [(129, 65), (256, 128), (257, 65), (511, 66), (512, 65), (513, 65), (1024, 65), (1025, 65)])
 @pytest.mark.parametrize("law", ["edges", "equal", "empty"])
 def test_every_sequence_in_its_turn(B, blocks, law):
     """More units than CUs over long tables, where the longer sequences are started first: every sequence is attended
