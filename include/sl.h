@@ -91,9 +91,10 @@ typedef struct sl_attn_desc {
                                    for a 4-bit one with head_dim 64 and more than 128
                                    sequences x KV heads, three for one with head_dim 128
                                    and at most 32, else, and for prefix-shared attention,
-                                   four per CU; none with a 4-bit cache and at most 128
-                                   blocks per sequence, a workgroup per sequence and KV
-                                   head, unless prefix sharing saves more);
+                                   four per CU; none with a 4-bit cache and at most 256
+                                   blocks per sequence (128 up to 64 sequences x KV heads),
+                                   a workgroup per sequence and KV head, unless prefix
+                                   sharing saves more);
                                    1..65536: exactly this many. The result does not depend
                                    on it beyond fp32 rounding; tests vary it to exercise
                                    the merge. */

@@ -174,47 +174,62 @@ sl_status resolve_workers(const sl_attn_desc *d, int kv, int *nw, bool prefix = 
 // slots are sized.
 int shared_workers(int nw) { return nw / 4 > 0 ? nw / 4 : 1; }
 
-// Wavefronts per unit if plain attention over a 4-bit cache runs as one workgroup
-// per unit (launch_unit_fp4), else 0: where the block table says that every
-// sequence is short. (The lengths themselves are not known here; a call with a
-// worker count of its own gets the workers.) Eight where the table is long and that
-// leaves every workgroup a CU. Calls, split and merge -> a workgroup per unit, MI355X, tokens
-// 1 .. 16 times the table's blocks:
-//   blocks                 16             64            128               256
-//   5 x 28/4 heads                   13.0 ->  8.0   12.4 ->  9.3
-//   64 x 28/4          13.1 ->  8.8  14.9 ->  8.6   17.3 -> 11.5   22.0 -> 19.0
-//   256 x 28/4                       26.5 -> 16.1   35.2 -> 27.6   57.4 -> 58.7
-//   512 x 64/8         36.4 -> 25.3  73.3 -> 56.7
-//   384 x 32/8, D = 64 20.1 -> 12.9  35.8 -> 25.5   53.2 -> 44.4   92.0 -> 87.0
-//   4 x 32/8, D = 64                                               12.9 -> 14.5
-// (512 x 64/8 of 16 blocks with eight wavefronts 42.6; up to 64 blocks eight gain nothing: 64 x 28/4 of 64
-// 8.6 and with four 8.5, 64 x 32/8, D = 64 of 48 8.2 and 7.6, 8 x 4/2, D = 64 of 16 4.8 and 4.4; of 128
-// blocks 64 x 28/4 11.7 and 12.7, 5 x 28/4 9.7 and 10.4.)
-int unit_waves(const sl_attn_desc *d, int kv)
+// Wavefronts per unit if attention over a 4-bit cache runs as one workgroup per
+// unit (launch_unit_fp4), else 0: where the block table says that every sequence is
+// short, at most 256 blocks, or 128 where there are few units. (The lengths
+// themselves are not known here; a call with a worker count of its own gets the
+// workers.) Eight where the table is long and that leaves every workgroup a CU. Calls,
+// split and merge -> a workgroup per unit, MI355X, cold pages, tokens 1 .. 16 times the
+// table's blocks:
+//   blocks                 16             64            128            256
+//   5 x 28/4 heads      8.7 ->  4.7    9.6 ->  7.2   10.6 ->  9.7   11.9 -> 14.5
+//   4 x 32/8, D = 64    8.0 ->  4.8    8.5 ->  6.7   10.1 ->  8.1   10.6 -> 11.8
+//   16 x 28/4                                                       15.3 -> 16.0
+//   32 x 28/4                                                       17.7 -> 16.4
+//   64 x 28/4          11.6 ->  5.4   15.3 ->  8.4   19.1 -> 11.6   24.9 -> 18.6
+//   256 x 28/4         17.9 ->  8.9   26.0 -> 17.8   36.6 -> 30.7   59.4 -> 55.3
+//   512 x 16/1                                                      46.2 -> 32.2
+//   384 x 32/8, D = 64 20.2 -> 13.0   37.6 -> 27.1   53.2 -> 44.4
+//   128 x 32/8, D = 64                                              36.3 -> 32.1
+// With 300 blocks both take the same, and lognormal lengths in such a table less as a
+// stream (180 x 28/4 27.3 -> 35.1).
+// (512 x 64/8 of 16 blocks with eight wavefronts 42.6 for 25.7; up to 64 blocks eight gain nothing:
+// 64 x 28/4 of 64 8.6 and with four 8.5, 64 x 32/8, D = 64 of 48 8.2 and 7.6, 8 x 4/2, D = 64 of 16
+// 4.8 and 4.4; of 128 blocks 64 x 28/4 11.7 and 12.7, 5 x 28/4 9.7 and 10.4.)
+constexpr int kUnitBlocksFew = 128, kFewUnits = 64;
+int unit_waves(const sl_attn_desc *d, int kv, bool prefix = false)
 {
-    if (kv != kFp4 || d->num_workers != 0 || d->max_blocks_per_seq > kUnitBlocks)
+    const long long units = (long long)d->batch * d->num_kv_heads;
+    const int most = prefix || units > kFewUnits ? kUnitBlocks : kUnitBlocksFew;
+    if (kv != kFp4 || d->num_workers != 0 || d->max_blocks_per_seq > most)
         return 0;
-    return (long long)d->batch * d->num_kv_heads <= 256 && d->max_blocks_per_seq > 64 ? 8 : 4;
+    return units <= 256 && d->max_blocks_per_seq > 64 ? 8 : 4;
 }
 
 // The same for prefix sharing. Reading the shared pages once costs the products of
 // 16-row blocks, the scans and a merge; attending every member by itself costs its
 // tiles again, out of the caches. Prefix kernel -> a workgroup per unit:
 //   prompts x samples of prompt, heads, D        units x blocks
-//   3 x 22 of 1000, 12/12, 64                         53064   16.4 -> 12.8
-//   8 x 8 of 500, 28/4, 128                           14592   21.1 ->  9.3
-//   16 x 16 of 1000, 28/4, 128                       121856   33.6 -> 21.7
-//   64 x 16 of 800, 28/4, 128                        258048   78.3 -> 54.6
-//   64 x 16 of 1800, 28/4, 128                       512000   98.7 -> 105.8
-//   128 x 4 of 500, 32/8, 64                         180224   37.1 -> 28.6
-//   16 x 16 of 1800, 32/8, 64                        256000   31.5 -> 33.9
+//   3 x 22 of 1000, 12/12, 64                         59400   17.0 -> 13.1
+//   8 x 8 of 500, 28/4, 128                           11264   18.6 ->  6.8
+//   16 x 16 of 1000, 28/4, 128                        76800   36.9 -> 18.2
+//   64 x 16 of 800, 28/4, 128                        258048   77.7 -> 54.4
+//   64 x 16 of 1800, 28/4, 128                       512000   96.2 -> 104.2
+//   128 x 4 of 500, 32/8, 64                         180224   36.6 -> 27.8
+//   16 x 16 of 1800, 32/8, 64                        256000   30.1 -> 31.9
+// and with more than 128 blocks:
+//   2 x 4 of 3600, 28/4, 128                           7520   19.9 -> 15.2
+//   4 x 8 of 3000, 28/4, 128                          25600   26.5 -> 13.4
+//   32 x 8 of 2200, 28/4, 128                        153600   42.2 -> 33.5
+//   8 x 3 of 3000, 32/8, 64                           38400   20.2 -> 11.3
+//   3 x 22 of 3000, 12/12, 64                        158400   19.0 -> 27.2
 // The pages were in the last-level cache, which favours reading them often; so the
 // limits lie below the sizes where both take the same.
 int unit_waves_prefix(const sl_attn_desc *d, int kv, int num_groups)
 {
-    const long long most = d->head_dim == 128 ? 400000 : 200000;
+    const long long most = (d->head_dim == 128 ? 400000 : 200000) / (d->max_blocks_per_seq > 128 ? 2 : 1);
     const bool few = (long long)d->batch * d->num_kv_heads * d->max_blocks_per_seq <= most;
-    return few && num_groups <= kUnitGroups ? unit_waves(d, kv) : 0;
+    return few && num_groups <= kUnitGroups ? unit_waves(d, kv, true) : 0;
 }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }

@@ -11,7 +11,7 @@
 // workgroups that all form the sums for themselves, if nothing that they read is
 // updated in place; else one workgroup moves the pages, and a second launch makes
 // the slot map. Bound by latency, a few dependent trips to memory: 256 requests of
-// one token 4.3 us.
+// one token 4.2 us.
 #include <algorithm>
 
 #include "sl_internal.h"
@@ -255,7 +255,7 @@ __global__ __launch_bounds__(kPageThreads) void release_pages_kernel(PageParams 
 }
 
 // Entries of the slot map, or of the block table, per workgroup, at least: one per
-// thread (66000 tokens of 96 requests 5.7 us, with four 8.4). Workgroups at most, one per
+// thread (66000 tokens of 96 requests 5.4 us, with four 8.4). Workgroups at most, one per
 // CU. Where one workgroup has to do everything, it makes the slot map too up to
 // this many entries.
 constexpr uint32_t kItemsPerBlock = kPageThreads;
@@ -269,8 +269,8 @@ bool apart(const PageParams &p) { return p.seq_lens_out != p.seq_lens && p.free_
 
 // (One request per thread where that is enough: the code for eight is four times
 // as long, and a first pass through it is instruction fetches.)
-// Call with 1024 requests of 1000 tokens: 11.4 us, with one workgroup for the
-// pages and a second launch 65; 96 of 1365: 11.2 and 14.6; 8192 of 100: 24 and 92.
+// Call with 1024 requests of 1000 tokens: 9.7 us, with one workgroup for the
+// pages and a second launch 63; 96 of 1365: 5.0 and 13.4; 8192 of 100: 23 and 85.
 hipError_t launch_extend_pages(const PageParams &p, hipStream_t stream)
 {
     const uint32_t tokens = (uint32_t)p.max_tokens;

@@ -316,10 +316,10 @@ inline size_t prefix_dynamic_lds(int batch, int max_sub)
     return sizeof(int32_t) * (3 * (size_t)batch + 2 * (size_t)max_sub + 3);
 }
 // Attention over a 4-bit cache with one workgroup per unit: tables of at most
-// this many blocks (at most 256, as each of four wavefronts keeps its run's
-// addresses in its lanes), tiles per step, and groups with shared pages (a
-// thread of the smaller workgroup each).
-constexpr int kUnitBlocks = 128;
+// this many blocks (each of four wavefronts keeps its run's addresses in its 64
+// lanes), tiles per step, and groups with shared pages (a thread of the smaller
+// workgroup each).
+constexpr int kUnitBlocks = 256;
 constexpr int kUnitStepTiles = 2;
 constexpr int kUnitGroups = 4 * kWave;
 struct UnitGroups {

@@ -179,7 +179,7 @@ def test_attention_sweep(i):
     assert_parity(out, reference(b, pool), f"sweep {i}")
 
 
-@pytest.mark.parametrize("blocks", [1, 2, 127, 128, 129, 300])
+@pytest.mark.parametrize("blocks", [1, 2, 127, 128, 129, 255, 256, 257, 300])
 @pytest.mark.parametrize("B,hq,hkv,d", [(3, 28, 4, 128), (70, 32, 8, 64), (7, 32, 2, 64), (300, 16, 1, 128)])
 def test_table_widths(B, hq, hkv, d, blocks):
     """Tables around the width where short sequences get a workgroup each: lengths of 0, 1, all of the table and others
@@ -206,7 +206,8 @@ def test_table_widths(B, hq, hkv, d, blocks):
     assert torch.equal(again[3:], out[3:])
 
 
-@pytest.mark.parametrize("B,blocks", [(129, 65), (256, 128), (257, 65), (511, 66), (512, 65), (513, 65), (1024, 65), (1025, 65)])
+@pytest.mark.parametrize("B,blocks", [(129, 65), (256, 128), (257, 65), (511, 66), (512, 65), (513, 65), (1024, 65), (1025, 65),
+                                      (65, 256), (130, 255), (200, 256)])
 @pytest.mark.parametrize("law", ["edges", "equal", "empty"])
 def test_every_sequence_in_its_turn(B, blocks, law):
     """More units than CUs over long tables, where the longer sequences are started first: every sequence is attended
@@ -430,9 +431,11 @@ def test_prefix_odd_groups():
 
 
 @pytest.mark.parametrize("case", [(3, 5, 2100, 28, 4, 128, 30, 200), (2, 9, 2070, 16, 4, 64, 20, 100),
-                                  (3, 3, 2050, 12, 12, 64, 30, 90), (300, 2, 40, 8, 2, 128, 10, 30)])
+                                  (3, 3, 2050, 12, 12, 64, 30, 90), (300, 2, 40, 8, 2, 128, 10, 30),
+                                  (2, 3, 3970, 28, 4, 128, 30, 126), (2, 3, 4090, 28, 4, 128, 30, 126),
+                                  (2, 5, 4000, 8, 2, 64, 30, 96), (2, 12, 4000, 12, 12, 64, 30, 96)])
 def test_prefix_past_the_short_tables(case):
-    """More than 128 blocks per sequence, or more than 256 groups."""
+    """More than 128 or 256 blocks per sequence, or more than 256 groups."""
     test_prefix_shapes(case, 0)
 
 
