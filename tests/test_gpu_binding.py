@@ -125,3 +125,38 @@ def test_workspace_of_a_stream_grows():
         got = [call(c) for c in (small, large, small, large)]
     torch.cuda.synchronize()
     assert all(torch.equal(x, want[i % 2]) for i, x in enumerate(got))
+
+
+def test_outputs_made_in_a_capture_and_in_inference_mode():
+    """Calls that make their own outputs, captured and replayed with eager calls between, and in inference mode."""
+    b, pool = make([300, 40, 17], 8, 2, 64, seed=5)
+    slots, one, count = _i32(3, 40, 5), _i32(1, 1, 1), _i32(30)
+    table = torch.cat([b.block_table, torch.zeros_like(b.block_table)], 1)
+    free = torch.arange(100, dtype=torch.int32, device=DEV)
+
+    def step():
+        lens, start, at, left = sl.pages_extend(b.seq_lens, one, table, free, count, 3)
+        return [sl.decode_attn_fp4(b.q, pool, b.block_table, b.seq_lens, b.scale), *sl.kv_read_fp4(slots, pool), lens,
+                start, at, left, *sl.pages_release(_zeros, b.seq_lens, table, free, count)]
+
+    _zeros = torch.zeros_like(one)
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        step()
+    stream.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=stream):
+        got = step()
+    for i in range(4):
+        b.q.mul_(0.5)
+        g.replay()
+        want = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, want, strict=True)), i
+    with torch.inference_mode():
+        here = step()
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(here, want, strict=True))
+    lens = want[3]
+    lens.add_(1)                       # an output is an ordinary tensor
+    assert lens.tolist() == [302, 42, 19]
