@@ -99,7 +99,18 @@ struct Fp4State {
     f32x4_t acc[HALF ? D / 32 : D / 16];
     f32x4_t l;   // the head's sum of weights, four times
     float m;
+    float ref;   // what a step's exponents are first taken against: m, or kBelowAll where |m| >= kWideScore
 };
+
+// An exponent in one fma, the exact product of score and factor minus m, has m's own
+// rounding error in it, since m is a rounded product: half a unit of its last place.
+// Below 2^24 that is at most half a binary order for all tokens alike, and cancels;
+// from 2^31 on it is 2^7 and more, and every weight would overflow or vanish. From
+// 2^24 on the product is therefore rounded before the subtraction. Such scores are
+// rare: a step meets them by comparing against kBelowAll, which no score is below and
+// so always sends it where the maximum is raised, and the step has no other branch.
+constexpr float kWideScore = 16777216.0f;
+constexpr float kBelowAll = -3.4028234663852886e38f;
 
 template <int D, bool HALF>
 __device__ __forceinline__ void reset(Fp4State<D, HALF> &st)
@@ -108,7 +119,7 @@ __device__ __forceinline__ void reset(Fp4State<D, HALF> &st)
     for (f32x4_t &a : st.acc)
         a = f32x4_t{0.f, 0.f, 0.f, 0.f};
     st.l = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    st.m = kNegInf;
+    st.m = st.ref = kNegInf;
 }
 
 template <int D, bool HALF>
@@ -168,17 +179,18 @@ __device__ __forceinline__ void fp4_step(Fp4State<D, HALF> &st, const T (&t)[N],
                                                             0, 0, 0);
     // Exponents relative to the running maximum as it is: |scale| log2(e) and the
     // subtraction in one fma. They show whether the maximum has to be raised, which
-    // compute_step asks of the scaled scores; then they are formed again.
+    // compute_step asks of the scaled scores; then they are formed again, for large
+    // scores in two roundings (kWideScore).
     // (Every score is read here, before any branch: this compiler has let a branch
     // over a few instructions lead from a matrix product to the first reader of its
     // result without the wait states in between.)
     float x[NT][4];
-    auto exponents = [&] {
+    auto exponents = [&](const auto &y, float factor, float from) {
 #pragma unroll
         for (int u = 0; u < NT; ++u)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                x[u][r] = __builtin_fmaf(s4[u][r], mul, -st.m);
+                x[u][r] = __builtin_fmaf(y[u][r], factor, -from);
     };
     auto mask = [&](auto &y) {
         if (partial) {
@@ -210,7 +222,7 @@ __device__ __forceinline__ void fp4_step(Fp4State<D, HALF> &st, const T (&t)[N],
             top = max3(top, y[i / 4][i % 4], i + 1 < 4 * NT ? y[(i + 1) / 4][(i + 1) % 4] : y[i / 4][i % 4]);
         return top;
     };
-    exponents();
+    exponents(s4, mul, st.ref);
     mask(x);
     if (__builtin_amdgcn_ballot_w64(largest_of(x) > kRescaleSlack) != 0) {
         mask(s4);
@@ -222,8 +234,15 @@ __device__ __forceinline__ void fp4_step(Fp4State<D, HALF> &st, const T (&t)[N],
                 a *= alpha;
             st.l *= alpha;
             st.m = mx;
+            st.ref = __builtin_fabsf(mx) < kWideScore ? mx : kBelowAll;
         }
-        exponents();
+        const bool wide = st.ref != st.m;
+#pragma unroll
+        for (int u = 0; u < NT; ++u)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                s4[u][r] = wide ? s4[u][r] * mul : s4[u][r];
+        exponents(s4, wide ? 1.0f : mul, st.m);
         mask(x);   // (a factor of zero made a masked score's NaN)
     }
     float p[NT][4];
