@@ -86,21 +86,46 @@ __global__ __launch_bounds__(kWave * kWavesPerBlock) void prefix_fp4_kernel(Spli
     }
 }
 
-// Whether this thread's group holds sequence b and shares more pages than its L
-// tokens fill: shared as scan_prefix_groups has it, in range and at or after the
-// end of every earlier group's range.
-__device__ __forceinline__ bool cut_short(const UnitGroups &g, const SplitParams &p, int b, int L)
+// The group that sequence b shares pages in, as scan_prefix_groups has it (in range
+// and at or after the end of every earlier group's range): its first member, whose
+// table entries stand for all members', and the pages, 0 where there is none. Every
+// wavefront looks at all groups, one per lane and pass, the passes' loads together.
+struct SharedIn {
+    int lead, pages;
+};
+__device__ __forceinline__ SharedIn shared_in(const UnitGroups &g, const SplitParams &p, int b, int lane)
 {
-    const int k = threadIdx.x;
-    if (k >= g.count)
-        return false;
-    const int lo = g.start[k], hi = g.start[k + 1], sp = g.shared_pages[k];
-    if (lo < 0 || b < lo || b >= hi || hi > p.batch || sp <= 0 || sp > p.max_blocks || L >= sp * kPageSize)
-        return false;
-    for (int j = 0; j < k; ++j)   // (only on the way to a NaN row)
-        if (g.start[j + 1] > lo)
-            return false;
-    return true;
+    constexpr int kPasses = kUnitGroups / kWave;
+    int lo[kPasses], hi[kPasses], sp[kPasses];
+    bool descends = false;
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i)
+        if (i * kWave < g.count) {
+            const int k = min(i * kWave + lane, g.count - 1);
+            lo[i] = g.start[k];
+            hi[i] = g.start[k + 1];
+            sp[i] = g.shared_pages[k];
+        }
+    SharedIn in = {b, 0};
+    auto holds = [&](int i) { return lo[i] >= 0 && b >= lo[i] && b < hi[i] && hi[i] <= p.batch && sp[i] > 0 && sp[i] <= p.max_blocks; };
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i)
+        if (i * kWave < g.count)
+            descends |= lo[i] > hi[i];
+    const bool ascending = __builtin_amdgcn_ballot_w64(descends) == 0;
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i)
+        if (i * kWave < g.count) {
+            bool here = holds(i);
+            if (!ascending && here)
+                for (int j = 0; j < min(i * kWave + lane, g.count - 1); ++j)
+                    here &= g.start[j + 1] <= lo[i];
+            if (const uint64_t mask = __builtin_amdgcn_ballot_w64(here)) {   // (groups with shared pages are disjoint)
+                const int at = __builtin_ctzll(mask);
+                in = {__builtin_amdgcn_readlane(lo[i], at), __builtin_amdgcn_readlane(sp[i], at)};
+            }
+        }
+    return in;
 }
 
 // The sequence that is number `turn` when those of the longest quarter of the
@@ -188,9 +213,9 @@ constexpr int kTurnBatch = kTurnPasses * kWavesPerBlock * kWave;
 // Steps of two tiles: with four, fewer workgroups fit a CU (384 x 1..1024, 32/8
 // heads, D = 64 28.8 us instead of 25.5; 512 x 1..256, 64/8 heads 40.3 and 25.3).
 // With prefix sharing the members' rows of a prompt are attended one by one too
-// (its pages come out of the caches): the groups only decide which member is
-// shorter than its group's shared pages. A thread looks at one group, in the
-// first trip to memory.
+// (its pages come out of the caches): the groups only decide whose table entries
+// name the shared pages, and which member is shorter than they are. They come in
+// the first trip to memory.
 template <int D, int KV, int WAVES, bool TURNS>
 __global__ __launch_bounds__(kWave * WAVES) void unit_fp4_kernel(SplitParams p, UnitGroups groups)
 {
@@ -209,6 +234,9 @@ __global__ __launch_bounds__(kWave * WAVES) void unit_fp4_kernel(SplitParams p, 
     } else {
         L = p.seq_lens[b];
     }
+    SharedIn shared = {b, 0};
+    if constexpr (!TURNS)   // (never with groups)
+        shared = shared_in(groups, p, b, lane);
     const int unit = b * Hkv + g;
     const int n = lane & 15, quad = lane >> 4;
     const int max_len = p.max_blocks * kPageSize;
@@ -217,10 +245,11 @@ __global__ __launch_bounds__(kWave * WAVES) void unit_fp4_kernel(SplitParams p, 
     const int tiles = min(count * NT, pages - first * NT);   // this wavefront's, at most kWave
     static_assert(kUnitBlocks <= WAVES * kWave, "a run's addresses lie in the lanes");
     // Lane i: the address of tile i of the run (those past it: the last one's).
-    const int page = p.block_table[(size_t)b * p.max_blocks + max(0, min(first * NT + min(lane, tiles - 1), pages - 1))];
+    const int block = max(0, min(first * NT + min(lane, tiles - 1), pages - 1));
+    const int page = p.block_table[(size_t)(block < shared.pages ? shared.lead : b) * p.max_blocks + block];
     const bool in = page >= 0 && page < p.num_pages;
-    const bool mine = cut_short(groups, p, b, L) || (lane < tiles && !in);
-    const bool bad = L < 0 || L > max_len || __builtin_amdgcn_ballot_w64(mine) != 0;
+    const bool bad = L < 0 || L > max_len || L < shared.pages * kPageSize ||
+                     __builtin_amdgcn_ballot_w64(lane < tiles && !in) != 0;
     const uint64_t record = reinterpret_cast<uint64_t>(p.k_pages) +
                             (in ? (uint64_t)(uint32_t)(page * Hkv + g) * (uint32_t)fp4_record_bytes(D) : 0u);
     u32x4_t q[D / 32];

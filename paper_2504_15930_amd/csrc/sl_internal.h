@@ -317,8 +317,7 @@ inline size_t prefix_dynamic_lds(int batch, int max_sub)
 }
 // Attention over a 4-bit cache with one workgroup per unit: tables of at most
 // this many blocks (each of four wavefronts keeps its run's addresses in its 64
-// lanes), tiles per step, and groups with shared pages (a thread of the smaller
-// workgroup each).
+// lanes), tiles per step, and groups with shared pages (four per lane).
 constexpr int kUnitBlocks = 256;
 constexpr int kUnitStepTiles = 2;
 constexpr int kUnitGroups = 4 * kWave;
