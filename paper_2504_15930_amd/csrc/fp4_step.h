@@ -236,13 +236,17 @@ __device__ __forceinline__ void fp4_step(Fp4State<D, HALF> &st, const T (&t)[N],
             st.m = mx;
             st.ref = __builtin_fabsf(mx) < kWideScore ? mx : kBelowAll;
         }
+        float factor = mul;
         const bool wide = st.ref != st.m;
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(wide) != 0, 0)) {
+            factor = wide ? 1.0f : mul;
 #pragma unroll
-        for (int u = 0; u < NT; ++u)
+            for (int u = 0; u < NT; ++u)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                s4[u][r] = wide ? s4[u][r] * mul : s4[u][r];
-        exponents(s4, wide ? 1.0f : mul, st.m);
+                for (int r = 0; r < 4; ++r)
+                    s4[u][r] = wide ? s4[u][r] * mul : s4[u][r];
+        }
+        exponents(s4, factor, st.m);
         mask(x);   // (a factor of zero made a masked score's NaN)
     }
     float p[NT][4];
