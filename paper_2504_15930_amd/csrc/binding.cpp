@@ -12,6 +12,7 @@
 // the current one): sl.py then makes the call step by step, which says what is wrong
 // or handles it.
 #include <c10/hip/HIPFunctions.h>
+#include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ATen.h>
@@ -133,15 +134,19 @@ bool float_of(PyObject *o, float &x)
 PyObject *given(PyObject *o) { return Py_NewRef(o); }
 PyObject *result(PyObject *o, const at::Tensor &made) { return o == Py_None ? THPVariable_Wrap(made) : given(o); }
 
-// The stream's workspace of at least `bytes`; undefined, with a Python error, where it could not be made.
+// The current stream's workspace of at least `bytes`, or one for this call alone if it is being captured (both
+// sl.py's to make); undefined, with a Python error, where it could not be made.
 at::Tensor workspace(int index, hipStream_t stream, size_t bytes)
 {
     const unsigned long long handle = reinterpret_cast<uintptr_t>(stream);
-    PyObject *key = Py_BuildValue("(iK)", index, handle);
-    PyObject *ws = key ? PyDict_GetItemWithError(g_workspaces, key) : nullptr;
-    Py_XDECREF(key);
-    if (ws && (size_t)THPVariable_Unpack(ws).numel() >= bytes)
-        return THPVariable_Unpack(ws);
+    PyObject *ws = nullptr;
+    if (c10::hip::currentStreamCaptureStatusMayInitCtx() == c10::hip::CaptureStatus::None) {
+        PyObject *key = Py_BuildValue("(iK)", index, handle);
+        ws = key ? PyDict_GetItemWithError(g_workspaces, key) : nullptr;
+        Py_XDECREF(key);
+        if (ws && (size_t)THPVariable_Unpack(ws).numel() >= bytes)
+            return THPVariable_Unpack(ws);
+    }
     ws = PyErr_Occurred() ? nullptr
                           : PyObject_CallFunction(g_make_workspace, "iKn", index, handle, (Py_ssize_t)bytes);
     if (!ws)

@@ -178,7 +178,13 @@ def _workspace(index: int, stream: int, nbytes: int) -> torch.Tensor:
     current stream). Calls on one stream run one after the other, so they may share a buffer;
     calls on two streams could overlap, so each stream gets its own. The buffer is allocated
     while its stream is current, so when it is replaced by a larger one torch's allocator hands
-    its memory out again only in that stream's order, after the kernels that used it."""
+    its memory out again only in that stream's order, after the kernels that used it.
+
+    A graph's replays are in no such order, and outlive the buffer that was cached when it was
+    captured. So a call that is being captured gets a buffer of its own, out of the graph's memory
+    pool: torch keeps that for as long as the graph, and shares it with no other graph unasked."""
+    if torch.cuda.is_current_stream_capturing():
+        return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=torch.device("cuda", index))
     key = (index, stream)
     ws = _workspaces.get(key)
     if ws is None or ws.numel() < nbytes:
@@ -259,6 +265,10 @@ def decode_attn(q, k_pages, v_pages, block_table, seq_lens, scale, *, out=None, 
 
     ``timing`` optionally holds two raw hipEvent handles recorded around the
     split-KV kernel. The call is asynchronous on the current stream.
+
+    ``workspace`` (uint8 on the GPU) is the call's scratch; without it, the current stream's, or,
+    captured by ``torch.cuda.graph``, memory of the graph's own pool. (A capture that was begun
+    past torch has no such pool: such calls need a ``workspace``.)
     """
     return _run(False, q, k_pages, v_pages, None, None, block_table, seq_lens, scale, out,
                 num_workers, workspace, timing)
@@ -523,8 +533,7 @@ def _run_fp4(q, kv_pages, block_table, seq_lens, scale, groups, out, num_workers
 def decode_attn_fp4(q, kv_pages, block_table, seq_lens, scale, *, out=None, num_workers=0, workspace=None,
                     timing=None) -> torch.Tensor:
     """``sl_decode_attn_fp4``: decode attention over a 4-bit cache, ``kv_pages`` uint8
-    [num_pages, Hkv, ``fp4_record_bytes(D)``]; otherwise as ``decode_attn``. (Without ``workspace`` a captured call
-    uses the capturing stream's: graphs whose replays may overlap each need one of their own.)"""
+    [num_pages, Hkv, ``fp4_record_bytes(D)``]; otherwise as ``decode_attn``."""
     if workspace is None and timing is None:
         done = (_fast or _binding()).attn(q, kv_pages, block_table, seq_lens, scale, None, None, out, num_workers)
         if done is not None:

@@ -1,0 +1,37 @@
+"""Which scratch buffer a Python call gets (on the host: torch's allocation and capture state are stood in for)."""
+import pytest
+import torch
+
+from paper_2504_15930_amd import sl
+
+
+@pytest.fixture
+def capturing(monkeypatch):
+    """A list whose first entry says whether the current stream is being captured; host buffers for device ones."""
+    state = [False]
+    empty = torch.empty
+    monkeypatch.setattr(sl.torch, "empty", lambda n, dtype, device: empty(n, dtype=dtype))
+    monkeypatch.setattr(sl.torch.cuda, "is_current_stream_capturing", lambda: state[0])
+    monkeypatch.setattr(sl, "_workspaces", {})
+    return state
+
+
+def test_a_stream_keeps_its_buffer_until_a_larger_one(capturing):
+    a = sl._workspace(0, 5, 1000)
+    assert sl._workspace(0, 5, 10) is a and sl._workspace(0, 5, 1000) is a
+    assert sl._workspace(0, 6, 1000) is not a and sl._workspace(1, 5, 1000) is not a
+    b = sl._workspace(0, 5, 1001)
+    assert b is not a and b.numel() >= 1001 and sl._workspace(0, 5, 1) is b
+
+
+def test_a_captured_call_gets_a_buffer_that_no_other_call_has(capturing):
+    """A graph holds its address: it is neither what eager calls on the stream use, nor dropped by them for a larger one,
+    nor another graph's."""
+    a = sl._workspace(0, 5, 1000)
+    capturing[0] = True
+    x, y = sl._workspace(0, 5, 1000), sl._workspace(0, 5, 10)
+    assert len({t.data_ptr() for t in (a, x, y)}) == 3 and x.numel() >= 1000 and y.numel() >= 10
+    sl._workspace(0, 7, 1000)
+    assert list(sl._workspaces.values()) == [a]     # nothing of a capture is kept for later calls
+    capturing[0] = False
+    assert sl._workspace(0, 5, 1000) is a
