@@ -39,7 +39,8 @@
  *    page_size, or whose live block-table entries name a page outside
  *    [0, num_pages), gets NaN in all its output rows.
  *  - Calls sharing one workspace must not overlap in time (e.g. run them on
- *    one stream).
+ *    one stream, and from one host thread at a time: a call enqueues several
+ *    kernels, between which another thread's could come).
  */
 #ifndef SL_H
 #define SL_H

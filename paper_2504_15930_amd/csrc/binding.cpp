@@ -37,7 +37,7 @@ struct Library {
     decltype(&sl_pages_release) release;
 } g_lib;
 
-// sl.py's workspaces, {(device, stream): tensor}, its function that makes one, and the one that raises for a status.
+// sl.py's workspaces, {(device, stream, thread): tensor}, its function that makes one, and the one that raises for a status.
 PyObject *g_workspaces = nullptr, *g_make_workspace = nullptr, *g_check = nullptr;
 
 constexpr int kPage = 16;
@@ -134,14 +134,14 @@ bool float_of(PyObject *o, float &x)
 PyObject *given(PyObject *o) { return Py_NewRef(o); }
 PyObject *result(PyObject *o, const at::Tensor &made) { return o == Py_None ? THPVariable_Wrap(made) : given(o); }
 
-// The current stream's workspace of at least `bytes`, or one for this call alone if it is being captured (both
-// sl.py's to make); undefined, with a Python error, where it could not be made.
+// This thread's workspace on the current stream, at least `bytes`, or one for this call alone if it is being captured
+// (both sl.py's to make); undefined, with a Python error, where it could not be made.
 at::Tensor workspace(int index, hipStream_t stream, size_t bytes)
 {
     const unsigned long long handle = reinterpret_cast<uintptr_t>(stream);
     PyObject *ws = nullptr;
     if (c10::hip::currentStreamCaptureStatusMayInitCtx() == c10::hip::CaptureStatus::None) {
-        PyObject *key = Py_BuildValue("(iK)", index, handle);
+        PyObject *key = Py_BuildValue("(iKk)", index, handle, PyThread_get_thread_ident());
         ws = key ? PyDict_GetItemWithError(g_workspaces, key) : nullptr;
         Py_XDECREF(key);
         if (ws && (size_t)THPVariable_Unpack(ws).numel() >= bytes)

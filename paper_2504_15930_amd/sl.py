@@ -12,6 +12,7 @@ import contextlib
 import ctypes
 import functools
 import os
+import threading
 
 import torch
 
@@ -170,13 +171,14 @@ def _prefix_workspace_bytes(index: int, num_groups: int, *sizes) -> int:
     return need.value
 
 
-_workspaces: dict[tuple[int, int], torch.Tensor] = {}
+_workspaces: dict[tuple[int, int, int], torch.Tensor] = {}
 
 
 def _workspace(index: int, stream: int, nbytes: int) -> torch.Tensor:
     """A cached scratch buffer of at least ``nbytes`` (256-byte aligned by torch) per (GPU,
-    current stream). Calls on one stream run one after the other, so they may share a buffer;
-    calls on two streams could overlap, so each stream gets its own. The buffer is allocated
+    current stream, host thread). Calls of one thread on one stream run one after the other, so they
+    may share a buffer; calls on two streams could overlap, and of two threads' calls on one stream
+    the kernels could alternate (a call is a split and a merge). The buffer is allocated
     while its stream is current, so when it is replaced by a larger one torch's allocator hands
     its memory out again only in that stream's order, after the kernels that used it.
 
@@ -185,7 +187,7 @@ def _workspace(index: int, stream: int, nbytes: int) -> torch.Tensor:
     pool: torch keeps that for as long as the graph, and shares it with no other graph unasked."""
     if torch.cuda.is_current_stream_capturing():
         return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=torch.device("cuda", index))
-    key = (index, stream)
+    key = (index, stream, threading.get_ident())
     ws = _workspaces.get(key)
     if ws is None or ws.numel() < nbytes:
         ws = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=torch.device("cuda", index))

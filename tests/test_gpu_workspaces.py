@@ -1,6 +1,8 @@
 """Scratch memory of calls without a ``workspace`` of their own, where it matters: calls of two kernels (split and merge)
 that are captured, replayed beside other calls and other graphs, or made on several streams. Every result equals, bit for
 bit, the same call alone (the kernels' results depend only on their inputs)."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -157,6 +159,36 @@ def test_two_streams_at_once(kind, way):
     torch.cuda.synchronize()
     for i, out in enumerate(got):
         assert _same(out, want[i % 2]), i
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_two_threads_on_one_stream(kind, way):
+    """Their calls' kernels may alternate on the stream."""
+    print("two threads", kind, way, flush=True)
+    calls = [_call(kind, 64, s, most=1500) for s in (1, 2)]
+    want = [call().clone() for _, call in calls]
+    outs = [[torch.empty_like(q) for _ in range(40)] for q, _ in calls]
+    torch.cuda.synchronize()
+    stream, start, errors = torch.cuda.Stream(), threading.Barrier(2), []
+
+    def work(i):
+        try:
+            with torch.cuda.stream(stream):
+                start.wait()
+                for out in outs[i]:
+                    calls[i][1](out)
+        except Exception as e:   # handed to the main thread
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(timeout=60)
+    assert not any(t.is_alive() for t in threads) and not errors, errors
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(_same(x, want[i]) for x in outs[i]), i
 
 
 @pytest.mark.parametrize("workers", [0, WORKERS])

@@ -1,4 +1,6 @@
 """Which scratch buffer a Python call gets (on the host: torch's allocation and capture state are stood in for)."""
+import threading
+
 import pytest
 import torch
 
@@ -35,3 +37,13 @@ def test_a_captured_call_gets_a_buffer_that_no_other_call_has(capturing):
     assert list(sl._workspaces.values()) == [a]     # nothing of a capture is kept for later calls
     capturing[0] = False
     assert sl._workspace(0, 5, 1000) is a
+
+
+def test_threads_on_one_stream_have_their_own(capturing):
+    """A call is two kernels, which another thread's could come between."""
+    mine, theirs = sl._workspace(0, 5, 1000), []
+    t = threading.Thread(target=lambda: theirs.extend(sl._workspace(0, 5, n) for n in (1000, 10, 2000)))
+    t.start()
+    t.join()
+    assert theirs[0] is theirs[1] and theirs[2] is not theirs[0] and all(x is not mine for x in theirs)
+    assert sl._workspace(0, 5, 1000) is mine
