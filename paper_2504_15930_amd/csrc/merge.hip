@@ -217,7 +217,9 @@ __global__ __launch_bounds__(kMergeThreads) void merge_kernel(MergeParams p)
 // unit area, at (first query row) / G. Rows finished by one worker with no
 // shared pages were written by the split kernel. A sequence shorter than its
 // group's shared prefix, or with an invalid length, gets a NaN row.
-template <int D>
+// FP4: a 4-bit cache, whose shared-page workers are counted by another rule (53
+// instructions that the others do not need).
+template <int D, bool FP4>
 __global__ __launch_bounds__(kMergeThreads) void merge_prefix_kernel(PrefixMergeParams p)
 {
     const int Hkv = p.num_kv_heads, G = p.group, Hq = p.num_q_heads;
@@ -238,7 +240,7 @@ __global__ __launch_bounds__(kMergeThreads) void merge_prefix_kernel(PrefixMerge
     const int ob = p.cum_own[b + 1] - co;
     const long long tot_o = (long long)p.cum_own[p.batch] * Hkv;
     const long long tot_s = (long long)p.cum_shared[p.max_sub] * Hkv;
-    const int per_block = p.kv == kFp4 ? p.cum_shared[p.max_sub + 1] : 1;   // shared-page workers
+    const int per_block = FP4 ? p.cum_shared[p.max_sub + 1] : 1;   // shared-page workers
     const bool bad = L < 0 || L > p.max_blocks * kPageSize || L < sk * kPageSize;
     if (sk == 0 && ob == 0) {
         const uint32_t fill = L < 0 ? 0x7fc07fc0u : 0u;   // bf16 NaN / +0
@@ -249,12 +251,12 @@ __global__ __launch_bounds__(kMergeThreads) void merge_prefix_kernel(PrefixMerge
     const int nw_o = effective_workers(tot_o, p.num_workers, p.step_tiles, wide_from(p.num_workers, p.kv));
     const int nw_s = effective_workers(
         tot_s,
-        p.kv == kFp4 ? shared_workers_of(effective_shared_workers_fp4(tot_o, tot_s, per_block, p.num_workers,
-                                                                      p.num_shared_workers, p.max_shared_workers,
-                                                                      p.step_tiles),
-                                         per_block, p.num_workers)
-                     : effective_shared_workers(tot_o, p.num_workers, p.num_shared_workers, p.max_shared_workers,
-                                                p.step_tiles, p.kv),
+        FP4 ? shared_workers_of(effective_shared_workers_fp4(tot_o, tot_s, per_block, p.num_workers,
+                                                             p.num_shared_workers, p.max_shared_workers,
+                                                             p.step_tiles),
+                                per_block, p.num_workers)
+            : effective_shared_workers(tot_o, p.num_workers, p.num_shared_workers, p.max_shared_workers,
+                                       p.step_tiles, p.kv),
         p.step_tiles, 0);
     const long long a_o = (long long)Hkv * co + (long long)g * ob;
     const long long a_s = (long long)Hkv * s_start + (long long)g * ss;
@@ -329,12 +331,15 @@ hipError_t launch_merge_prefix(const PrefixMergeParams &p, int head_dim, hipStre
 {
     const int per_block = kMergeThreads / kWave;
     const dim3 grid((unsigned)((p.num_q_heads + per_block - 1) / per_block), (unsigned)p.batch);
+    using Kernel = void (*)(PrefixMergeParams);
+    Kernel kernel = nullptr;
     if (head_dim == 128)
-        hipLaunchKernelGGL(merge_prefix_kernel<128>, grid, dim3(kMergeThreads), 0, stream, p);
+        kernel = p.kv == kFp4 ? merge_prefix_kernel<128, true> : merge_prefix_kernel<128, false>;
     else if (head_dim == 64)
-        hipLaunchKernelGGL(merge_prefix_kernel<64>, grid, dim3(kMergeThreads), 0, stream, p);
-    else
+        kernel = p.kv == kFp4 ? merge_prefix_kernel<64, true> : merge_prefix_kernel<64, false>;
+    if (!kernel)
         return hipErrorInvalidValue;
+    hipLaunchKernelGGL(kernel, grid, dim3(kMergeThreads), 0, stream, p);
     return hipGetLastError();
 }
 
