@@ -574,6 +574,21 @@ sl_status check_pages(const sl_attn_desc *d)
 
 }  // namespace
 
+sl_status workspace_bytes(const sl_attn_desc *d, int last, size_t *bytes)
+{
+    sl_status st = check_desc(d);
+    int nw = 0;
+    for (int kv = kBf16; kv <= last && st == SL_OK; ++kv) {
+        int n = 0;
+        st = resolve_workers(d, kv, &n);
+        nw = n > nw ? n : nw;
+    }
+    if (st == SL_OK)
+        *bytes = workspace_layout(nullptr, d->batch, d->max_blocks_per_seq, d->num_kv_heads,
+                                  d->num_q_heads / d->num_kv_heads, d->head_dim, nw, nullptr);
+    return st;
+}
+
 sl_status decode_attn_then_append(const sl_attn_desc *d, const uint16_t *q, const void *k_pages, const void *v_pages,
                                   const float *k_scales, const float *v_scales, const int32_t *block_table,
                                   const int32_t *seq_lens, float scale, uint16_t *out, bool fp8,
@@ -626,18 +641,7 @@ sl_status sl_decode_attn_workspace_size(const sl_attn_desc *desc, size_t *bytes)
     if (!bytes)
         return SL_ERR_NULL;
     // Sized for the largest of the three caches' worker counts, so one workspace serves them all.
-    int nw = 0;
-    for (int kv = sl::kBf16; kv <= sl::kFp4; ++kv) {
-        int n = 0;
-        st = sl::resolve_workers(desc, kv, &n);
-        if (st != SL_OK)
-            return st;
-        nw = n > nw ? n : nw;
-    }
-    *bytes = sl::workspace_layout(nullptr, desc->batch, desc->max_blocks_per_seq,
-                                  desc->num_kv_heads, desc->num_q_heads / desc->num_kv_heads,
-                                  desc->head_dim, nw, nullptr);
-    return SL_OK;
+    return sl::workspace_bytes(desc, sl::kFp4, bytes);
 }
 
 sl_status sl_decode_attn(const sl_attn_desc *desc, const uint16_t *q, const uint16_t *k_pages,

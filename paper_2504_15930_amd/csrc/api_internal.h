@@ -16,4 +16,7 @@ sl_status decode_attn_then_append(const sl_attn_desc *d, const uint16_t *q, cons
                                   const int32_t *seq_lens, float scale, uint16_t *out, bool fp8,
                                   const AppendParams *next);
 
+// Workspace bytes of sl_decode_attn and its siblings for the caches kBf16 .. `last` (Kv). Checks `d`, not `bytes`.
+sl_status workspace_bytes(const sl_attn_desc *d, int last, size_t *bytes);
+
 }  // namespace sl

@@ -394,7 +394,7 @@ sl_status sl_engine_create(const sl_engine_config *cfg, const sl_engine_buffers 
     *out = nullptr;
     const sl_attn_desc &d = bufs->desc;
     size_t need = 0;
-    sl_status st = sl_decode_attn_workspace_size(&d, &need);   // validates the descriptor
+    sl_status st = sl::workspace_bytes(&d, sl::kE4m3, &need);   // validates the descriptor (the engine has no 4-bit cache)
     if (st != SL_OK)
         return st;
     if (!d.workspace || d.workspace_bytes < need || !aligned(d.workspace, 256))
