@@ -9,8 +9,9 @@
 //
 // Every function returns None, with nothing launched, for a call that is not the plain
 // case (an argument of another type, shape, layout or device, a device that is not
-// the current one): sl.py then makes the call step by step, which says what is wrong
-// or handles it.
+// the current one, a torch dispatch mode, which is to see the outputs made): sl.py
+// then makes the call step by step, which says what is wrong or handles it.
+#include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPStream.h>
@@ -175,7 +176,7 @@ template <PyObject *(*F)(PyObject *const *), int ARGS>
 PyObject *guarded(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     try {
-        PyObject *const r = n == ARGS ? F(a) : nullptr;
+        PyObject *const r = n == ARGS && !c10::impl::TorchDispatchModeTLS::any_modes_set() ? F(a) : nullptr;
         if (r || PyErr_Occurred())
             return r;
     } catch (...) {
