@@ -13,6 +13,7 @@ import ctypes
 import functools
 import os
 import threading
+import warnings
 
 import torch
 
@@ -483,11 +484,24 @@ _BAD_SIZES = (AttributeError, IndexError, TypeError, ValueError)   # what asking
 _fast = None
 
 
+class _NoBinding:
+    """In place of a binding that does not load: declines every call."""
+
+    def __getattr__(self, name):
+        return lambda *args: None
+
+
 def _binding():
     global _fast
     if _fast is None:
         lib = load()
-        from . import _binding as fast
+        try:
+            from . import _binding as fast
+        except ImportError as e:   # not built, or for another torch
+            warnings.warn(f"calls of the 4-bit cache and the page bookkeeping take 4 to 6 us more: no _binding.so ({e}); "
+                          "build it with `python -m paper_2504_15930_amd.build`", RuntimeWarning, stacklevel=3)
+            _fast = _NoBinding()
+            return _fast
         names = ("sl_decode_attn_fp4", "sl_decode_attn_prefix_fp4", "sl_decode_attn_workspace_size",
                  "sl_decode_attn_prefix_workspace_size", "sl_kv_append_fp4", "sl_kv_write_fp4", "sl_kv_read_fp4",
                  "sl_pages_extend", "sl_pages_release")
