@@ -8,6 +8,7 @@ import pytest
 
 from paper_2504_15930_amd import build, sl
 from test_kernel_resources import LDS_PER_CU, _code_objects, sizes, static_lds   # noqa: F401 (fixtures)
+from test_matrix_waits import early_reads
 
 
 def _lds(static_lds, name, count):
@@ -70,3 +71,24 @@ def test_the_other_caches_merge_does_not_count_4_bit_workers(listings, D):
     size = {fp4: len([k for n, b in listings.items() if f"merge_prefix_kernelILi{D}ELb{fp4}E" in n for k in b.splitlines()])
             for fp4 in (0, 1)}
     assert 0 < size[0] < size[1]
+
+
+def test_products_leave_their_results_in_ordinary_registers(listings):
+    """The check of the wait states after matrix products (test_matrix_waits.py) follows v registers: no result may be in
+    an accumulation register, whose readers it would not see. (The compiler may move other values there and back.)"""
+    seen = 0
+    for name, body in listings.items():
+        for operands in re.findall(r"^\s+v_s?mfma\S* (.*?)\s*//", body, re.M):
+            seen += 1
+            assert re.fullmatch(r"v\[\d+:\d+\]", operands.split(", ")[0]), (name, operands)
+    assert seen > 100
+
+
+def test_products_of_every_kernel_are_read_after_their_wait(listings):
+    """The other caches' kernels too."""
+    kernels = {name: body for name, body in listings.items() if "v_mfma" in body}
+    assert {k for k in ("split_kv_kernel", "prefix_split_kernel", "split_fp4_kernel", "prefix_fp4_kernel", "unit_fp4_kernel")
+            if any(k in name for name in kernels)} == {"split_kv_kernel", "prefix_split_kernel", "split_fp4_kernel",
+                                                       "prefix_fp4_kernel", "unit_fp4_kernel"}
+    for name, body in kernels.items():
+        assert not early_reads(body), name
