@@ -233,3 +233,48 @@ def test_a_captured_decode_step_with_pages_rows_and_both_attentions(workers, way
         torch.cuda.synchronize()
         assert all(torch.equal(s[n], eager[n]) for n in s), i
         assert all(_same(x, y) for x, y in zip(outs, want)), i
+
+
+@pytest.mark.parametrize("own_stream", [False, True])
+@pytest.mark.parametrize("kind", ["bf16", "fp4", "prefix_fp4"])
+def test_eager_calls_of_another_thread_during_a_capture(kind, own_stream, way):
+    """Their stream is not being captured: they keep their own buffer, and the graph its."""
+    print("another thread during a capture", kind, own_stream, way, flush=True)
+    calls = [_call(kind, 64, s, most=900) for s in (1, 2)]
+    want = [call().clone() for _, call in calls]
+    outs = [torch.empty_like(q) for q, _ in calls]
+    # (torch's streams come round: two made one after the other are different ones)
+    captured, other = torch.cuda.Stream(), torch.cuda.Stream()
+    stream = other if own_stream else torch.cuda.default_stream()
+    errors, warm, go = [], threading.Event(), threading.Event()
+
+    def work():
+        try:
+            with torch.cuda.stream(stream):
+                calls[1][1](outs[1])      # makes the thread's buffer, before the capture
+                stream.synchronize()
+                outs[1].zero_()
+                warm.set()
+                assert go.wait(30)
+                for _ in range(3):
+                    calls[1][1](outs[1])
+        except Exception as e:            # handed to the main thread
+            errors.append(e)
+            warm.set()
+
+    t = threading.Thread(target=work)
+    t.start()
+    assert warm.wait(30)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=captured, capture_error_mode="thread_local"):
+        calls[0][1](outs[0])
+        go.set()
+        t.join(30)
+    assert not t.is_alive() and not errors, errors
+    torch.cuda.synchronize()
+    assert _same(outs[1], want[1])
+    outs[0].zero_()
+    g.replay()
+    torch.cuda.synchronize()
+    assert _same(outs[0], want[0])
