@@ -109,7 +109,8 @@ typedef struct sl_attn_desc {
 
 /*
  * Bytes of workspace the calls need for `desc`, whichever the cache (sizes and
- * num_workers; no pointer is read). With num_workers == 0 this queries the current device.
+ * num_workers; no pointer is read): with num_workers == 0 the largest of the caches'
+ * defaults decides, and a call on one cache may need less. With num_workers == 0 this queries the current device.
  * Errors: SL_ERR_NULL, SL_ERR_SHAPE, SL_ERR_UNSUPPORTED, SL_ERR_HIP.
  */
 sl_status sl_decode_attn_workspace_size(const sl_attn_desc *desc, size_t *bytes);
@@ -342,7 +343,9 @@ sl_status sl_kv_read_fp4(const sl_attn_desc *desc, const uint8_t *kv_pages, cons
 /*
  * Page bookkeeping on the GPU, for a paged cache of any type: block tables and
  * slot maps from the requests' lengths, without a trip to the host (the decode
- * engine of sl_engine.h keeps its own on the host).
+ * engine of sl_engine.h keeps its own on the host). The slot map is what
+ * sl_kv_write_fp4 and sl_kv_read_fp4 take; rows of the other caches go in through
+ * the block table (sl_kv_append, sl_kv_append_fp8).
  *
  * The free pages are a stack: the first free_count[0] entries of free_pages,
  * taken from and returned to its end.

@@ -142,10 +142,12 @@ sl_status resolve_workers(const sl_attn_desc *d, int kv, int *nw, bool prefix = 
     // with three per four CUs 132; with one tile per step 132 and 150). Two waves per SIMD
     // were slower for all but E4M3 with head_dim 64 and one tile per step.
     // A 4-bit cache with head_dim 64 takes two per CU: its tiles are so short that
-    // instructions set the pace, and one wavefront's fill the other's waits (384
-    // sequences of 1..2048 tokens, 32/8 heads: 52.4 us, with one 60.7). With head_dim
-    // 128 two were slower (512 x 512 + lognormal(2048), 28/4 heads: 174 us with one,
-    // 187 with two; 256 of 64/8 heads 350 and 367).
+    // instructions set the pace, and one wavefront's fill the other's waits (64
+    // sequences of 1..8192 tokens, 32/8 heads: 42.3 us with one, 36.7 with two; 200 of
+    // 1..4800 65.6 and 60.7; 384 of 4800 at most, lognormal, 12/12 heads 81.0 and 67.0; 20
+    // of 1..16384, 32/8 27.1 and 27.4). With head_dim 128 a workgroup's registers fill
+    // a CU, and a second half of the workers only starts behind the first (256 of 1..6400,
+    // 28/4 heads: 83.4 us, with twice the workers 93.0; 128 of 1..8192, 64/8 105 and 114).
     // With few units (sequences x KV heads) the merge of every worker's pieces weighs more than
     // the last workers' share of the stream: up to 32 units three workgroups per four CUs take
     // less with head_dim 128 (4 x 1..16384 tokens, 28/4 heads 18.5 -> 17.0 us, 2 of 64/8 18.1 ->
@@ -178,7 +180,8 @@ int shared_workers(int nw) { return nw / 4 > 0 ? nw / 4 : 1; }
 // unit (launch_unit_fp4), else 0: where the block table says that every sequence is
 // short, at most 256 blocks, or 128 where there are few units. (The lengths
 // themselves are not known here; a call with a worker count of its own gets the
-// workers.) Eight where the table is long and that leaves every workgroup a CU. Calls,
+// workers.) Eight where the table is long and that leaves every workgroup a CU (slower with
+// 3072 units and more, below; between 257 and those it was not measured). Calls,
 // split and merge -> a workgroup per unit, MI355X, cold pages, tokens 1 .. 16 times the
 // table's blocks:
 //   blocks                 16             64            128            256

@@ -5,12 +5,13 @@
 // workgroup per unit for short sequences (unit_fp4_kernel). A step of the streams
 // is four tiles, with prefix sharing two (17 D bytes each, K and V).
 //
-// Measured (MI355X, split and merge, cold pages): 512 x 512 + lognormal(2048)
-// tokens, 28/4 heads of 128, 1.07 GB of records in 174 us, 6.2 TB/s (reading such
+// Measured (MI355X, cold pages), split and merge: 512 x 512 + lognormal(2048)
+// tokens, 28/4 heads of 128, 1.07 GB of records in 173 us, 6.2 TB/s (reading such
 // records at random without any arithmetic 6.7); 256 sequences of 64/8 heads, 2.26
-// GB in 350 us, 6.4 TB/s: bound by HBM. With head_dim 64 a record is half as long
-// for the same loads, scales and softmax: 384 x 1..2048, 32/8 heads, 0.21 GB in
-// 42.3 us, 4.9 TB/s, the VALUs busy for half of it.
+// GB in 351 us, 6.4 TB/s: bound by HBM. With head_dim 64 a record is half as long
+// for the same loads, scales and softmax: 64 x 1..8192, 32/8 heads, in 36.7 us; a
+// workgroup per unit, 384 x 1..2048, 32/8 heads, 0.21 GB in 41.4 us, 5.0 TB/s, the
+// VALUs busy for half of it.
 #include "prefix_unit.h"
 
 namespace sl {
@@ -207,8 +208,8 @@ constexpr int kTurnBatch = kTurnPasses * kWavesPerBlock * kWave;
 // Attention where every sequence is short (a block table of at most
 // kUnitBlocks entries): one workgroup per unit, its tiles dealt to the wavefronts
 // in contiguous runs of whole steps, their states combined in LDS. One launch, no
-// scan of the batch, no partial states in memory, two trips to memory before the
-// first product (length and table entries, then records and query rows). Bound by
+// scan of the batch, no partial states in memory, three trips to memory before the
+// first product (length, table entries, records beside query rows). Bound by
 // that latency, and with thousands of units by instructions, as the stream is.
 // Steps of two tiles: with four, fewer workgroups fit a CU (384 x 1..1024, 32/8
 // heads, D = 64 28.8 us instead of 25.5; 512 x 1..256, 64/8 heads 40.3 and 25.3).

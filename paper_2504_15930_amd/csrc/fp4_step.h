@@ -21,7 +21,9 @@
 //   zeros for odd ones, the others the other way round. Half of the operand is
 //   zeros in place of the columns that would be empty, the permutes are gone (16
 //   of some 70 vector instructions per tile of D = 128), and the accumulators are
-//   half as many, which leaves room for a second wavefront per SIMD.
+//   half as many: unit_fp4_kernel with D = 128 has four wavefronts per SIMD in place
+//   of three (114 registers, not 160). The streams have as many as without it, one with
+//   D = 128 (280 and 320) and two with D = 64.
 //
 // The sum of the weights comes out of the matrix product too: a row of ones times
 // the weights. They enter rounded to bf16 as they do the value product, so the

@@ -647,7 +647,8 @@ def pages_extend(seq_lens, new_tokens, block_table, free_pages, free_count, max_
     ``free_pages`` [num_pages] (the first ``free_count`` [1] of it are free) and are entered in ``block_table``, in
     place. Returns ``(seq_lens_out, token_start, slots, free_count_out)``: the new lengths [B], where each request's
     tokens begin in the slot map [B + 1], the slot map [max_tokens] (-1 past the last token), and the pages left.
-    ``seq_lens_out`` and ``free_count_out`` may be the inputs themselves. All int32; asynchronous."""
+    ``seq_lens_out`` and ``free_count_out`` may be the inputs themselves. All int32; asynchronous. (Four outputs made by
+    the call lie in one allocation, which lasts as long as any of them: clone one that is kept when the slot map is not.)"""
     done = (_fast or _binding()).extend(seq_lens, new_tokens, block_table, free_pages, free_count, max_tokens,
                                         seq_lens_out, free_count_out, token_start, slots)
     if done is not None:
@@ -689,8 +690,9 @@ def pages_extend(seq_lens, new_tokens, block_table, free_pages, free_count, max_
 
 def pages_release(finished, seq_lens, block_table, free_pages, free_count, *, seq_lens_out=None, free_count_out=None):
     """``sl_pages_release``: the pages of requests with ``finished`` [B] not 0 go back on the stack, in place, and
-    their lengths become 0. Returns ``(seq_lens_out, free_count_out)``, which may be the inputs themselves. A page that
-    several rows share would come back once for each: keep such pages out of the released rows."""
+    their lengths become 0. Returns ``(seq_lens_out, free_count_out)``, which may be the inputs themselves, or, made by
+    the call, lie in one allocation. A page that several rows share would come back once for each: keep such pages out of
+    the released rows."""
     done = (_fast or _binding()).release(finished, seq_lens, block_table, free_pages, free_count, seq_lens_out,
                                          free_count_out)
     if done is not None:
