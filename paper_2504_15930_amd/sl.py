@@ -191,6 +191,11 @@ def _workspace(index: int, stream: int, nbytes: int) -> torch.Tensor:
     key = (index, stream, threading.get_ident())
     ws = _workspaces.get(key)
     if ws is None or ws.numel() < nbytes:
+        if ws is None:   # a new stream or thread: those of ended threads go
+            alive = {t.ident for t in threading.enumerate()} | {key[2]}
+            for k in list(_workspaces):
+                if k[2] not in alive:
+                    _workspaces.pop(k, None)
         ws = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=torch.device("cuda", index))
         _workspaces[key] = ws
     return ws

@@ -47,3 +47,22 @@ def test_threads_on_one_stream_have_their_own(capturing):
     t.join()
     assert theirs[0] is theirs[1] and theirs[2] is not theirs[0] and all(x is not mine for x in theirs)
     assert sl._workspace(0, 5, 1000) is mine
+
+
+def test_an_ended_threads_buffers_go(capturing):
+    """Not at once: with the next buffer that is made."""
+    mine = sl._workspace(0, 5, 1000)
+    inside, done = threading.Event(), threading.Event()
+    alive = threading.Thread(target=lambda: (sl._workspace(0, 5, 1000), inside.set(), done.wait(30)))
+    ended = threading.Thread(target=lambda: [sl._workspace(0, s, 1000) for s in (5, 6, 7)])
+    alive.start()                 # (before the other ends, whose number it could be given)
+    assert inside.wait(30)
+    ended.start()
+    ended.join()
+    assert len(sl._workspaces) == 5
+    sl._workspace(1, 5, 1000)
+    threads = {k[2] for k in sl._workspaces}
+    assert threads == {threading.get_ident(), alive.ident} and len(sl._workspaces) == 3
+    assert sl._workspace(0, 5, 1000) is mine
+    done.set()
+    alive.join()
