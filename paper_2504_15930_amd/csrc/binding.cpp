@@ -4,8 +4,8 @@
 // The kernels of a small step take 3 to 5 us, so what the host spends per call
 // counts: checks of four to nine tensors, the outputs, the descriptor and a ctypes
 // call took 4 to 7 us in Python, beside the 3 us of the launch. Here the tensors are
-// read directly (append 7.6 us per call -> 3.9, with outputs to make attention 9.6 ->
-// 5.4, pages_extend 11.6 -> 5.5).
+// read directly (append 7.5 us per call -> 3.6, with outputs to make attention 9.9 ->
+// 5.3, pages_extend 11.4 -> 5.2).
 //
 // Every function returns None, with nothing launched, for a call that is not the plain
 // case (an argument of another type, shape, layout or device, a device that is not

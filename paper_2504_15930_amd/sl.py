@@ -484,8 +484,8 @@ _BAD_SIZES = (AttributeError, IndexError, TypeError, ValueError)   # what asking
 
 # csrc/binding.cpp, bound to the library that ``load`` gives. Each of its functions makes one call of its kind on
 # contiguous tensors of the current device, without timing events, and returns None, nothing done, for any other; the
-# Python below then makes it, or says what is wrong with it. Time per call, 8 requests: attention 9.6 us by Python
-# alone, 5.4 here; append 7.6 and 3.9, read 9.5 and 5.3, pages_extend 11.6 and 5.5, pages_release 10.5 and 5.1.
+# Python below then makes it, or says what is wrong with it. Time per call, 8 requests: attention 9.9 us by Python
+# alone, 5.3 here; append 7.5 and 3.6, read 9.5 and 5.1, pages_extend 11.4 and 5.2, pages_release 10.2 and 4.9.
 _fast = None
 
 
