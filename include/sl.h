@@ -109,8 +109,9 @@ typedef struct sl_attn_desc {
 
 /*
  * Bytes of workspace the calls need for `desc`, whichever the cache (sizes and
- * num_workers; no pointer is read): with num_workers == 0 the largest of the caches'
- * defaults decides, and a call on one cache may need less. With num_workers == 0 this queries the current device.
+ * num_workers; no pointer is read). With num_workers == 0 this queries the
+ * current device, and the largest of the caches' defaults decides: a call on
+ * one cache may need less.
  * Errors: SL_ERR_NULL, SL_ERR_SHAPE, SL_ERR_UNSUPPORTED, SL_ERR_HIP.
  */
 sl_status sl_decode_attn_workspace_size(const sl_attn_desc *desc, size_t *bytes);

@@ -181,7 +181,7 @@ int shared_workers(int nw) { return nw / 4 > 0 ? nw / 4 : 1; }
 // short, at most 256 blocks, or 128 where there are few units. (The lengths
 // themselves are not known here; a call with a worker count of its own gets the
 // workers.) Eight where the table is long and that leaves every workgroup a CU (slower with
-// 3072 units and more, below; between 257 and those it was not measured). Calls,
+// 384 x 8 units and more, below; between 257 and those it was not measured). Calls,
 // split and merge -> a workgroup per unit, MI355X, cold pages, tokens 1 .. 16 times the
 // table's blocks:
 //   blocks                 16             64            128            256
